@@ -26,6 +26,7 @@
 #ifndef BALANCEKV_H_
 #define BALANCEKV_H_
 
+#include <stddef.h>
 #include <stdint.h>
 
 #ifdef __cplusplus
@@ -194,6 +195,62 @@ int balancekv_decode_attn_static(const void* K, const void* V, int n_streams, in
  * `stream` and the shared one -- it counts as one of the calls that the shared block's users order --, and with
  * status 1 all of it.  Allocates nothing; synchronises `stream`, with status 1 the device.  The paper has no counterpart. */
 int balancekv_decode_attn_static_status(int* status_host, void* stream);
+
+/* Operators on caches that the caller holds.  The paper has no counterpart: they are what a serving program does next to
+ * BalanceKV -- attend a prompt or a token and keep count of the weight that every cached row receives, keep the rows that
+ * received the most, and attend a (compressed) prefix that a batch of sequences shares.
+ *
+ * All three take device memory that the caller owns, contiguous as stated, K, V, q and outputs 16-byte aligned; dtype 0 =
+ * float32, 1 = bfloat16; head_dim 64 or 128; group (query heads per KV head) 1..8.  lens (device, may be NULL: every row is in
+ * use) holds the rows in use, of which a call attends no more than the capacity.  Rows behind the last may hold anything;
+ * the rows in use are finite.  Each call works in a workspace of the caller (device, 256-byte aligned, at least the bytes that the
+ * _workspace call of the same arguments gives on the host; contents need not be kept or cleared).  Calls that may overlap, graph replays
+ * among them, need workspaces of their own.  Nothing is allocated and nothing synchronised; every call may be captured.  Memory that a
+ * call writes overlaps nothing else that it is given, unless stated.  Errors: BALANCEKV_E_INVAL for bad arguments,
+ * BALANCEKV_E_NOMEM for too small a workspace, BALANCEKV_E_CUDA. */
+
+/* Attention of the newest n_queries tokens of every stream over its cache, and the weight that each cached row receives:
+ *   p[h,j,i] = e^{<k_i,q_hj>/sqrt d} / sum_{i' <= len - n_queries + j} e^{<k_i',q_hj>/sqrt d},   i <= len - n_queries + j,
+ *   out[h,j,:] = sum_i p[h,j,i] v_i,
+ *   score_out[i] = decay score_in[i] + sum_h sum_{j >= n_queries - n_scored} p[h,j,i]        for i < len.
+ * The last n_queries rows in use are the queries' own tokens, in order: query j sees the rows up to its own (one query: all of
+ * them).  A query ahead of the first row (len < n_queries, a padded sequence) sees nothing: its output is zero.
+ * K, V: [n_streams, capacity, head_dim]   q, out: [n_streams, group, n_queries, head_dim]   score_in (may be NULL: zeros),
+ * score_out (may be score_in): float32 [n_streams, capacity]; scores behind the last row stay as they are.  n_scored: the newest queries
+ * that count, 0 .. n_queries; with 0 the scores are not touched and may be NULL. */
+int balancekv_attn_scored(const void* K, const void* V, const int32_t* lens, int n_streams, int capacity, const void* q, void* out,
+                          int n_queries, int group, int head_dim, int dtype, const float* score_in, float* score_out, int n_scored,
+                          float decay, void* workspace, size_t workspace_bytes, void* stream);
+int balancekv_attn_scored_workspace(int n_streams, int capacity, int n_queries, int group, int head_dim, int dtype, int n_scored,
+                                    size_t* bytes);
+
+/* Keep n_keep rows of every stream: first those at positions below n_first and the newest n_recent positions (pos > newest -
+ * n_recent; n_first + n_recent <= n_keep), then those of the largest scores; among equal scores the lowest row (-0 equals 0,
+ * NaN is below every number).  A stream of at most n_keep rows keeps them all.  Kept rows below row n_keep stay where they are, and the
+ * kept rows behind it fill the holes, both in ascending order: the fewest rows move, and positions tell a row's age from then on.
+ * K, V: [n_streams, capacity, head_dim]   score: float32, pos (may be NULL: the row's number): int32, both [n_streams, capacity]
+ * K_out, V_out: [n_streams, capacity_out, head_dim], score_out, pos_out (may be NULL) [n_streams, capacity_out], capacity_out >=
+ * min(n_keep, capacity); rows behind the kept ones stay as they are.  lens_out (may be NULL, may be lens): the rows kept.
+ * In place: K_out = K, V_out = V, score_out = score, pos_out = pos (NULL and NULL too), capacity_out = capacity; only the rows
+ * that fill holes are copied -- per token, with one row over the budget, at most one. */
+int balancekv_cache_evict(const void* K, const void* V, const float* score, const int32_t* pos, const int32_t* lens, int n_streams,
+                          int capacity, void* K_out, void* V_out, float* score_out, int32_t* pos_out, int32_t* lens_out, int capacity_out,
+                          int n_keep, int n_first, int n_recent, int head_dim, int dtype, void* workspace, size_t workspace_bytes,
+                          void* stream);
+int balancekv_cache_evict_workspace(int n_streams, int capacity, int n_keep, int head_dim, int dtype, int in_place, size_t* bytes);
+
+/* Decode attention of a batch whose sequences share a prefix, which is read once for all of them: per sequence and query head
+ *   out = (sum_{prefix} w_i e^{<k_i,q>/sqrt d} v_i + sum_{own rows} e^{<k_i,q>/sqrt d} v_i)
+ *       / (sum_{prefix} w_i e^{<k_i,q>/sqrt d}     + sum_{own rows} e^{<k_i,q>/sqrt d}),
+ * Theorem 3.3's estimator where the prefix is a compressed stream (rows and weights as balancekv_cache_view gives them).
+ * K_prefix, V_prefix: [n_kv_heads, prefix_len, head_dim], prefix_len >= 1; w_prefix (may be NULL: ones): float32 [n_kv_heads,
+ * prefix_len], >= 0; a row of weight 0 counts as absent whatever it holds.  K, V: [n_seqs, n_kv_heads, capacity, head_dim], capacity >= 0
+ * (0: no own rows, K and V may be NULL); lens: [n_seqs].  q, out: [n_seqs, n_kv_heads * group, head_dim]. */
+int balancekv_decode_attn_prefix(const void* K_prefix, const void* V_prefix, const float* w_prefix, int prefix_len, const void* K,
+                                 const void* V, const int32_t* lens, int capacity, const void* q, void* out, int n_seqs,
+                                 int n_kv_heads, int group, int head_dim, int dtype, void* workspace, size_t workspace_bytes, void* stream);
+int balancekv_decode_attn_prefix_workspace(int prefix_len, int capacity, int n_seqs, int n_kv_heads, int group, int head_dim, int dtype,
+                                           size_t* bytes);
 
 /* Load an already-compressed set into level `level` of every stream of one layer
  * (weight 2^level, the weights of Theorem 3.3's estimator): K, V: [n_seqs, n_kv_heads,

@@ -5,6 +5,9 @@ from .binding import (  # noqa: E402,F401
     Context,
     EXPORTS,
     LIB_PATH,
+    attn_scored,
+    cache_evict,
+    decode_attn_prefix,
     decode_attn_static,
     decode_attn_static_status,
     load,
