@@ -55,9 +55,47 @@ __device__ inline void score_put(const ScoreArgs& S, int64_t at, float sum) {
   S.out[at] = S.in ? fmaf(S.decay, S.in[at], sum) : sum;
 }
 
+// A warp per query row: the slots' sums brought to one maximum and added, in the order of the slots.
+template <bool kBf16, int D>
+__device__ inline void join_splits(const AttnRows& A, int64_t row, int lane) {
+  float top = -INFINITY;
+  for (int i = lane; i < A.n_slots; i += 32) top = fmaxf(top, A.part_ml[(int64_t)i * A.total_rows + row].x);
+  top = warp_max(top);
+  const float base = top == -INFINITY ? 0.f : top;
+  constexpr int kPer = D / 32;
+  float sum = 0.f, acc[kPer] = {};
+#pragma unroll 4
+  for (int i = 0; i < A.n_slots; ++i) {
+    const int64_t at = (int64_t)i * A.total_rows + row;
+    const float2 ml = A.part_ml[at];
+    const float f = exp2f(ml.x - base);
+    sum = fmaf(ml.y, f, sum);
+#pragma unroll
+    for (int c = 0; c < kPer; c += 2) {
+      const float2 v = *reinterpret_cast<const float2*>(A.part + at * D + kPer * lane + c);
+      acc[c] = fmaf(v.x, f, acc[c]);
+      acc[c + 1] = fmaf(v.y, f, acc[c + 1]);
+    }
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  if (A.lse && lane == 0) A.lse[row] = sum == 0.f ? INFINITY : base + log2f(sum);
+#pragma unroll
+  for (int c = 0; c < kPer; c += 2) {
+    if constexpr (kBf16)
+      *reinterpret_cast<__nv_bfloat162*>(static_cast<__nv_bfloat16*>(A.out) + row * D + kPer * lane + c) = __floats2bfloat162_rn(acc[c] * inv, acc[c + 1] * inv);
+    else
+      *reinterpret_cast<float2*>(static_cast<float*>(A.out) + row * D + kPer * lane + c) = make_float2(acc[c] * inv, acc[c + 1] * inv);
+  }
+}
+
 cudaError_t launch_attn_simt(const AttnRows& A, int d, int is_bf16, cudaStream_t st);
 cudaError_t launch_attn_combine(const AttnRows& A, int d, int is_bf16, cudaStream_t st);
 cudaError_t launch_score_simt(const AttnRows& A, const ScoreArgs& S, int d, int is_bf16, cudaStream_t st);
+
+int few_splits(int64_t streams, int cap);
+int64_t few_pitch(int cap);
+cudaError_t launch_attn_few(const AttnRows& A, float* x, int d, int is_bf16, cudaStream_t st);
+cudaError_t launch_few_end(const AttnRows& A, float* x, const ScoreArgs& S, int d, int is_bf16, cudaStream_t st);
 
 struct EvictArgs {
   const void *K, *V;

@@ -49,7 +49,8 @@ void take_parts(AttnRows& A, Pieces& ws, int d) {
 
 // ---- attn_scored
 
-int plan_scored(AttnRows& A, Pieces& ws, int n_streams, int capacity, int n_queries, int group, int head_dim, int dtype, int n_scored) {
+// x: the logits that the one-pass kernels leave for the scores.
+int plan_scored(AttnRows& A, float*& x, Pieces& ws, int n_streams, int capacity, int n_queries, int group, int head_dim, int dtype, int n_scored) {
   if (n_streams < 1 || capacity < 1 || n_queries < 1 || group < 1 || group > kMaxGroup || !shape_ok(head_dim, dtype)) return BALANCEKV_E_INVAL;
   if (n_scored < 0 || n_scored > n_queries) return BALANCEKV_E_INVAL;
   const int64_t rows = (int64_t)group * n_queries;
@@ -62,9 +63,11 @@ int plan_scored(AttnRows& A, Pieces& ws, int n_streams, int capacity, int n_quer
   A.n_queries = n_queries;
   A.total_rows = (int)rows * n_streams;
   A.scale = (float)(1.4426950408889634 / std::sqrt((double)head_dim));
-  A.n_slots = A.splits = simt_splits((rows + 63) / 64 * n_streams, capacity);
+  const bool few = rows <= kFewRows;
+  A.n_slots = A.splits = few ? few_splits(n_streams, capacity) : simt_splits((rows + 63) / 64 * n_streams, capacity);
   take_parts(A, ws, head_dim);
   if (n_scored) A.lse = ws.take<float>(A.total_rows);
+  x = n_scored && few ? ws.take<float>(A.total_rows * few_pitch(capacity)) : nullptr;
   return BALANCEKV_OK;
 }
 
@@ -89,7 +92,7 @@ int plan_prefix(AttnRows& P, AttnRows& A, Pieces& ws, int prefix_len, int capaci
   A.lens_div = n_kv_heads;
   A.cap = capacity;
   A.n_rows = A.q_stream = A.q_inner = group;
-  A.splits = capacity ? simt_splits(streams, capacity) : 0;
+  A.splits = capacity ? few_splits(streams, capacity) : 0;
   A.slot0 = P.splits;
   P.n_slots = A.n_slots = P.splits + A.splits;
   take_parts(P, ws, head_dim);
@@ -121,8 +124,9 @@ extern "C" int balancekv_attn_scored_workspace(int n_streams, int capacity, int 
                                                size_t* bytes) {
   if (!bytes) return BALANCEKV_E_INVAL;
   AttnRows A{};
+  float* x;
   Pieces ws{nullptr};
-  const int rc = plan_scored(A, ws, n_streams, capacity, n_queries, group, head_dim, dtype, n_scored);
+  const int rc = plan_scored(A, x, ws, n_streams, capacity, n_queries, group, head_dim, dtype, n_scored);
   if (rc == BALANCEKV_OK) *bytes = ws.used;
   return rc;
 }
@@ -135,8 +139,9 @@ extern "C" int balancekv_attn_scored(const void* K, const void* V, const int32_t
       !aligned(workspace, 256))
     return BALANCEKV_E_INVAL;
   AttnRows A{};
+  float* x;
   Pieces ws{static_cast<char*>(workspace)};
-  if (const int rc = plan_scored(A, ws, n_streams, capacity, n_queries, group, head_dim, dtype, n_scored)) return rc;
+  if (const int rc = plan_scored(A, x, ws, n_streams, capacity, n_queries, group, head_dim, dtype, n_scored)) return rc;
   if (ws.used && !workspace) return BALANCEKV_E_INVAL;
   if (workspace_bytes < ws.used) return BALANCEKV_E_NOMEM;
   A.K = K;
@@ -145,9 +150,17 @@ extern "C" int balancekv_attn_scored(const void* K, const void* V, const int32_t
   A.q = q;
   A.out = out;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  cudaError_t e = launch_attn_simt(A, head_dim, dtype, st);
-  if (e == cudaSuccess && A.n_slots > 1) e = launch_attn_combine(A, head_dim, dtype, st);
-  if (e == cudaSuccess && n_scored) e = launch_score_simt(A, ScoreArgs{score_in, score_out, decay, n_scored}, head_dim, dtype, st);
+  const ScoreArgs S{score_in, score_out, decay, n_scored};
+  cudaError_t e;
+  if (A.n_rows <= kFewRows) {
+    e = launch_attn_few(A, x, head_dim, dtype, st);
+    if (e == cudaSuccess && n_scored) e = launch_few_end(A, x, S, head_dim, dtype, st);
+    else if (e == cudaSuccess && A.n_slots > 1) e = launch_attn_combine(A, head_dim, dtype, st);
+  } else {
+    e = launch_attn_simt(A, head_dim, dtype, st);
+    if (e == cudaSuccess && A.n_slots > 1) e = launch_attn_combine(A, head_dim, dtype, st);
+    if (e == cudaSuccess && n_scored) e = launch_score_simt(A, S, head_dim, dtype, st);
+  }
   return report("balancekv_attn_scored", e);
 }
 
@@ -183,7 +196,7 @@ extern "C" int balancekv_decode_attn_prefix(const void* K_prefix, const void* V_
   P.out = A.out = out;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t e = launch_attn_simt(P, head_dim, dtype, st);
-  if (e == cudaSuccess && A.splits) e = launch_attn_simt(A, head_dim, dtype, st);
+  if (e == cudaSuccess && A.splits) e = launch_attn_few(A, nullptr, head_dim, dtype, st);
   if (e == cudaSuccess && P.n_slots > 1) e = launch_attn_combine(P, head_dim, dtype, st);
   return report("balancekv_decode_attn_prefix", e);
 }

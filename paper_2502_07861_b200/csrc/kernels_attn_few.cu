@@ -1,0 +1,525 @@
+// Attention of up to eight query rows per stream over a caller-held cache: one pass at memory speed, split over the rows.
+//
+//   x_{r,i} = <q_r, k_i> log2(e) / sqrt d,   out_r = sum_i 2^(x_{r,i} - m_r) v_i / sum_i 2^(x_{r,i} - m_r)
+//
+// and where the rows are scored, the weights of every cached row: they need the finished sums of all splits, so the logits leave as
+// fp32 (4 bytes per row and query against 2 d elements read) and a second launch turns them into weights while it joins the splits.
+//
+// A CTA is four warps, each with a ring of its own of tiles of 32 rows that TMA fills (K and V tiles in turn, boxes of 128 bytes x
+// 32 rows, 128-byte swizzle): a warp waits for nothing but its own copies, and the lane that asks for the next tile does so as soon as
+// its warp has read the last.  bf16 tiles go through mma.sync with the cached rows as the M dimension and the queries as the eight
+// columns; fp32 tiles through FFMA, a lane per row for the logits and d / 32 columns per lane for the sums.
+// A bounded wait that gives up makes the results NaN.
+#include <algorithm>
+
+#include "attn_rows.cuh"
+#include "tma_mma.cuh"
+
+namespace bkv {
+
+namespace {
+
+using namespace mma;
+
+constexpr int kWarps = 4, kThreads = 32 * kWarps;
+constexpr int kTile = 32;                        // rows
+constexpr uint32_t kBox = kTile * 128;           // bytes
+
+template <bool kBf16, int D>
+struct Few {
+  static constexpr int kEsz = kBf16 ? 2 : 4, kBoxDims = 128 / kEsz, kBoxes = D / kBoxDims;
+  static constexpr uint32_t kTileBytes = kBoxes * kBox;
+  static constexpr int kRing = kTileBytes == 4096 ? 6 : 3;                   // tiles of a warp in flight
+  static constexpr int kCtas = kTileBytes == 16384 ? 1 : 2;                  // that share an SM
+  static constexpr int kPitch = D + 4;                                       // of a row in the merge buffer: sums, maximum, sum of weights
+  static constexpr size_t kSmem = 1024 + (size_t)kWarps * kRing * kTileBytes;
+  static_assert(kWarps * kFewRows * kPitch * 4 <= (int)(kWarps * kRing * kTileBytes), "the merge buffer takes the rings' place");
+};
+
+struct FewArgs {
+  AttnRows A;
+  float* x;               // [n_streams, n_rows, pitch] logits; null: not wanted
+  int64_t pitch;
+};
+
+// This warp's tiles of the CTA's share: every fourth of [t0, t1) from t0 + warp on.  Tile number n of the warp has the ring's
+// entries 2 n (K) and 2 n + 1 (V).
+template <bool kBf16, int D>
+struct Ring {
+  using F = Few<kBf16, D>;
+  const CUtensorMap *mk, *mv;
+  unsigned char* tiles;
+  uint64_t* full;
+  int stream, first_tile, entries;
+
+  __device__ void issue(int e) const {           // one lane
+    const CUtensorMap* map = e & 1 ? mv : mk;
+    const int s = e % F::kRing, row = (first_tile + (e >> 1) * kWarps) * kTile;
+    tc::mbar_expect_tx(full + s, F::kTileBytes);
+#pragma unroll
+    for (int b = 0; b < F::kBoxes; ++b) tma_load_3d(tiles + s * F::kTileBytes + b * kBox, map, b * F::kBoxDims, row, stream, full + s);
+  }
+  __device__ void start(int lane) const {
+    if (lane == 0)
+      for (int e = 0; e < min(F::kRing, entries); ++e) issue(e);
+  }
+  __device__ bool wait(int e, int lane, int* abort_flag) const {
+    bool ok = true;
+    if (lane == 0) ok = tc::wait_bar(full + e % F::kRing, (uint32_t)(e / F::kRing) & 1u, abort_flag);
+    ok = __shfl_sync(0xffffffffu, ok, 0);
+    __syncwarp();
+    return ok;
+  }
+  __device__ void next(int e, int lane) const {  // entry e has been read by the whole warp
+    __syncwarp();
+    if (lane == 0 && e + F::kRing < entries) issue(e + F::kRing);
+  }
+  // A wait gave up: the copies behind entry e that have been asked for are waited for, within limits, before the ring is left.
+  __device__ void drain(int e, int lane) const {
+    if (lane != 0) return;
+    const long long t0 = clock64();
+    for (int i = e; i < min(e + F::kRing, entries); ++i)
+      while (!tc::mbar_try_wait(full + i % F::kRing, (uint32_t)(i / F::kRing) & 1u) && clock64() - t0 < tc::kWaitCycles) {}
+  }
+  __device__ const unsigned char* at(int e) const { return tiles + e % F::kRing * F::kTileBytes; }
+};
+
+// Byte offset of 16-byte piece p of a row.
+__device__ inline uint32_t tile_off(int row, int piece) {
+  return (uint32_t)(piece >> 3) * kBox + (uint32_t)row * 128u + (uint32_t)(((piece & 7) ^ (row & 7)) << 4);
+}
+
+// The warp's sums of its tiles, to mrg[row][kPitch].
+template <int D>
+__device__ inline void few_warp_bf16(const FewArgs& P, const Ring<true, D>& R, int s, int len, int n_tiles, int lane, int* abort_flag, float* mrg, bool& failed) {
+  const AttnRows& A = P.A;
+  const int g = A.n_rows;
+  // With up to four rows the columns 4-7 repeat the rows 0-3, and in the second product they carry the low parts of the weights:
+  // one MMA then does what takes two with more rows.
+  const bool packed = g <= 4;
+  const int hq = lane >> 2, tq = lane & 3;       // C fragment: cached rows hq, hq + 8; query rows 2 tq, 2 tq + 1
+  uint32_t qb[D / 16][2];
+  {
+    const int hr = packed ? hq & 3 : hq;
+    const __nv_bfloat16* qp = static_cast<const __nv_bfloat16*>(A.q) + (hr < g ? attn_row(A, s, hr) : 0) * D;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {
+      qb[ks][0] = hr < g ? *reinterpret_cast<const uint32_t*>(qp + ks * 16 + 2 * tq) : 0u;
+      qb[ks][1] = hr < g ? *reinterpret_cast<const uint32_t*>(qp + ks * 16 + 8 + 2 * tq) : 0u;
+    }
+  }
+  int limit[2];
+  float* xs[2];
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const int h = packed ? (2 * tq + e) & 3 : 2 * tq + e;
+    limit[e] = h < g ? attn_limit(A, len, h) : 0;
+    xs[e] = P.x && 2 * tq + e < g ? P.x + ((int64_t)s * g + h) * P.pitch : nullptr;
+  }
+  constexpr int kMB = D / 16;
+  float o[kMB][4];                               // dim 16 mb + hq + 8 (j >> 1), query row 2 tq + (j & 1)
+#pragma unroll
+  for (int n = 0; n < kMB; ++n) { o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f; }
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+  const int mi = lane >> 3, mr = lane & 7;
+  const int k_row = (mi & 1) * 8 + mr, k_piece = mi >> 1;
+  const int v_row = (mi >> 1) * 8 + mr, v_piece = mi & 1;
+  for (int n = 0; n < n_tiles; ++n) {
+    const int row0 = (R.first_tile + n * kWarps) * kTile, rows = min(kTile, len - row0);
+    if (!R.wait(2 * n, lane, abort_flag)) { R.drain(2 * n, lane); failed = true; break; }
+    const uint32_t Kt = tc::smem_u32(R.at(2 * n));
+    float sa[2][4][4];
+#pragma unroll
+    for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) { sa[tb][c][0] = sa[tb][c][1] = sa[tb][c][2] = sa[tb][c][3] = 0.f; }
+#pragma unroll
+    for (int kh = 0; kh < D / 64; ++kh) {
+      uint32_t ka[4][2][4];
+#pragma unroll
+      for (int k4 = 0; k4 < 4; ++k4)
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb) ldsm_x4(Kt + tile_off(k_row + 16 * tb, (kh * 4 + k4) * 2 + k_piece), ka[k4][tb]);
+#pragma unroll
+      for (int k4 = 0; k4 < 4; ++k4)
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb) mma_bf16(sa[tb][k4], ka[k4][tb], qb[kh * 4 + k4][0], qb[kh * 4 + k4][1]);
+    }
+    R.next(2 * n, lane);
+    float x[2][4], mx[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+    for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int row = row0 + 16 * tb + hq + 8 * (j >> 1);
+        x[tb][j] = row < limit[j & 1] ? ((sa[tb][0][j] + sa[tb][1][j]) + (sa[tb][2][j] + sa[tb][3][j])) * A.scale : -INFINITY;
+        if (xs[j & 1] && row < len) xs[j & 1][row] = x[tb][j];
+        mx[j & 1] = fmaxf(mx[j & 1], x[tb][j]);
+      }
+#pragma unroll
+    for (int off = 4; off < 32; off <<= 1) {
+      mx[0] = fmaxf(mx[0], __shfl_xor_sync(0xffffffffu, mx[0], off));
+      mx[1] = fmaxf(mx[1], __shfl_xor_sync(0xffffffffu, mx[1], off));
+    }
+    if (__any_sync(0xffffffffu, mx[0] > m[0] || mx[1] > m[1])) {
+      float a[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float mn = fmaxf(m[e], mx[e]);
+        a[e] = mn == -INFINITY ? 0.f : exp2f(m[e] - mn);
+        l[e] *= a[e];
+        m[e] = mn;
+      }
+#pragma unroll
+      for (int i = 0; i < kMB; ++i) { o[i][0] *= a[0]; o[i][1] *= a[1]; o[i][2] *= a[0]; o[i][3] *= a[1]; }
+    }
+    const float base[2] = {m[0] == -INFINITY ? 0.f : m[0], m[1] == -INFINITY ? 0.f : m[1]};
+    // The weights enter the second product as bf16, split into a high and a low part (16 bits), so that the error stays that of the
+    // final rounding.
+    uint32_t bh[2][2], bl[2][2];
+#pragma unroll
+    for (int tb = 0; tb < 2; ++tb) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[tb][j] = exp2f(x[tb][j] - base[j & 1]);
+      l[0] += x[tb][0] + x[tb][2];
+      l[1] += x[tb][1] + x[tb][3];
+      const uint32_t ph0 = pack_bf16(x[tb][0], x[tb][1]), ph1 = pack_bf16(x[tb][2], x[tb][3]);
+      const uint32_t pl0 = pack_bf16(x[tb][0] - bf16_lo(ph0), x[tb][1] - bf16_hi(ph0));
+      const uint32_t pl1 = pack_bf16(x[tb][2] - bf16_lo(ph1), x[tb][3] - bf16_hi(ph1));
+      bh[tb][0] = movm_trans(packed && tq >= 2 ? pl0 : ph0);
+      bh[tb][1] = movm_trans(packed && tq >= 2 ? pl1 : ph1);
+      bl[tb][0] = packed ? 0u : movm_trans(pl0);
+      bl[tb][1] = packed ? 0u : movm_trans(pl1);
+    }
+    if (!R.wait(2 * n + 1, lane, abort_flag)) { R.drain(2 * n + 1, lane); failed = true; break; }
+    const uint32_t Vt = tc::smem_u32(R.at(2 * n + 1));
+#pragma unroll
+    for (int tb = 0; tb < 2; ++tb) {
+      const int row = min(v_row + 16 * tb, rows - 1);      // behind the last row that row again, times zero: what is there may be anything
+      uint32_t va[kMB][4];
+#pragma unroll
+      for (int mb = 0; mb < kMB; ++mb) ldsm_x4_trans(Vt + tile_off(row, mb * 2 + v_piece), va[mb]);
+#pragma unroll
+      for (int mb = 0; mb < kMB; ++mb) mma_bf16(o[mb], va[mb], bh[tb][0], bh[tb][1]);
+      if (!packed) {
+#pragma unroll
+        for (int mb = 0; mb < kMB; ++mb) mma_bf16(o[mb], va[mb], bl[tb][0], bl[tb][1]);
+      }
+    }
+    R.next(2 * n + 1, lane);
+  }
+#pragma unroll
+  for (int off = 4; off < 32; off <<= 1) {
+    l[0] += __shfl_xor_sync(0xffffffffu, l[0], off);
+    l[1] += __shfl_xor_sync(0xffffffffu, l[1], off);
+  }
+  if (packed) {
+#pragma unroll
+    for (int n = 0; n < kMB; ++n)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[n][j] += __shfl_xor_sync(0xffffffffu, o[n][j], 2);
+  }
+  __syncthreads();                               // every warp is done with its ring
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const int h = 2 * tq + e;
+    if (h >= g) continue;
+    float* to = mrg + h * Few<true, D>::kPitch;
+#pragma unroll
+    for (int n = 0; n < kMB; ++n) { to[16 * n + hq] = o[n][e]; to[16 * n + 8 + hq] = o[n][2 + e]; }
+    if (hq == 0) { to[D] = m[e]; to[D + 1] = l[e]; }
+  }
+}
+
+// The same with FFMA; kR >= n_rows rows.  qs: [kR][D], ps: [kR][32] of this warp.
+template <int D, int kR>
+__device__ inline void few_warp_fp32(const FewArgs& P, const Ring<false, D>& R, int s, int len, int n_tiles, int lane, int* abort_flag, const float* qs, float* ps,
+                                     float* mrg, bool& failed) {
+  const AttnRows& A = P.A;
+  const int g = A.n_rows;
+  constexpr int kC = D / 32;                     // columns of a lane: kC lane ..
+  float o[kR][kC], m[kR], l[kR];
+  int limit[kR];
+#pragma unroll
+  for (int r = 0; r < kR; ++r) {
+    m[r] = -INFINITY;
+    l[r] = 0.f;
+    limit[r] = r < g ? attn_limit(A, len, r) : 0;
+#pragma unroll
+    for (int c = 0; c < kC; ++c) o[r][c] = 0.f;
+  }
+  for (int n = 0; n < n_tiles; ++n) {
+    const int row0 = (R.first_tile + n * kWarps) * kTile, rows = min(kTile, len - row0), row = row0 + lane;
+    if (!R.wait(2 * n, lane, abort_flag)) { R.drain(2 * n, lane); failed = true; break; }
+    const unsigned char* Kt = R.at(2 * n);
+    float2 acc[kR];
+#pragma unroll
+    for (int r = 0; r < kR; ++r) acc[r] = make_float2(0.f, 0.f);
+#pragma unroll 4
+    for (int c = 0; c < D / 4; ++c) {
+      const float4 k = *reinterpret_cast<const float4*>(Kt + tile_off(lane, c));
+#pragma unroll
+      for (int r = 0; r < kR; ++r) {
+        const float4 q = *reinterpret_cast<const float4*>(qs + r * D + 4 * c);
+        acc[r] = __ffma2_rn(make_float2(k.x, k.y), make_float2(q.x, q.y), acc[r]);
+        acc[r] = __ffma2_rn(make_float2(k.z, k.w), make_float2(q.z, q.w), acc[r]);
+      }
+    }
+    R.next(2 * n, lane);
+    float x[kR];
+    bool more = false;
+#pragma unroll
+    for (int r = 0; r < kR; ++r) {
+      x[r] = row < limit[r] ? (acc[r].x + acc[r].y) * A.scale : -INFINITY;
+      if (P.x && r < g && row < len) P.x[((int64_t)s * g + r) * P.pitch + row] = x[r];
+      more = more || x[r] > m[r];
+    }
+    if (__any_sync(0xffffffffu, more)) {
+#pragma unroll
+      for (int r = 0; r < kR; ++r) {
+        const float mn = fmaxf(m[r], warp_max(x[r])), a = mn == -INFINITY ? 0.f : exp2f(m[r] - mn);
+        m[r] = mn;
+        l[r] *= a;
+#pragma unroll
+        for (int c = 0; c < kC; ++c) o[r][c] *= a;
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < kR; ++r) {
+      const float p = exp2f(x[r] - (m[r] == -INFINITY ? 0.f : m[r]));
+      l[r] += p;
+      ps[r * 32 + lane] = p;
+    }
+    if (!R.wait(2 * n + 1, lane, abort_flag)) { R.drain(2 * n + 1, lane); failed = true; break; }        // (a warp barrier too: the weights are there)
+    const unsigned char* Vt = R.at(2 * n + 1);
+    auto value = [&](int t, float (&v)[kC]) {
+      const unsigned char* at = Vt + tile_off(t, lane * kC / 4) + (lane * kC % 4) * 4;
+      if constexpr (kC == 4) {
+        const float4 w = *reinterpret_cast<const float4*>(at);
+        v[0] = w.x; v[1] = w.y; v[2] = w.z; v[3] = w.w;
+      } else {
+        const float2 w = *reinterpret_cast<const float2*>(at);
+        v[0] = w.x; v[1] = w.y;
+      }
+    };
+    auto add = [&](const float (&v)[kC], int r, float p) {
+#pragma unroll
+      for (int c = 0; c < kC; c += 2) {
+        const float2 y = __ffma2_rn(make_float2(v[c], v[c + 1]), make_float2(p, p), make_float2(o[r][c], o[r][c + 1]));
+        o[r][c] = y.x;
+        o[r][c + 1] = y.y;
+      }
+    };
+    if (rows == kTile) {
+#pragma unroll 2
+      for (int t = 0; t < kTile; t += 4) {
+        float v[4][kC];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) value(t + i, v[i]);
+#pragma unroll
+        for (int r = 0; r < kR; ++r) {
+          const float4 p = *reinterpret_cast<const float4*>(ps + r * 32 + t);
+          add(v[0], r, p.x);
+          add(v[1], r, p.y);
+          add(v[2], r, p.z);
+          add(v[3], r, p.w);
+        }
+      }
+    } else {
+      for (int t = 0; t < rows; ++t) {           // nothing behind the last row: what is there may be anything
+        float v[kC];
+        value(t, v);
+#pragma unroll
+        for (int r = 0; r < kR; ++r) add(v, r, ps[r * 32 + t]);
+      }
+    }
+    R.next(2 * n + 1, lane);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < kR; ++r) {
+    if (r >= g) break;
+    float* to = mrg + r * Few<false, D>::kPitch;
+#pragma unroll
+    for (int c = 0; c < kC; ++c) to[lane * kC + c] = o[r][c];
+    const float sum = warp_sum(l[r]);
+    if (lane == 0) { to[D] = m[r]; to[D + 1] = sum; }
+  }
+}
+
+// kR: rows that the fp32 form takes (bf16: 8).
+template <bool kBf16, int D, int kR>
+__global__ void __launch_bounds__(kThreads, (Few<kBf16, D>::kCtas)) attn_few_kernel(const __grid_constant__ FewArgs P, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv) {
+  using F = Few<kBf16, D>;
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ uint64_t full[kWarps][F::kRing];
+  __shared__ int abort_flag;
+  __shared__ __align__(16) float qs[kBf16 ? 4 : kR * D];
+  __shared__ __align__(16) float ps[kBf16 ? 4 : kWarps * kR * 32];
+  unsigned char* tiles = smem_raw + (-tc::smem_u32(smem_raw) & 1023u);
+  const AttnRows& A = P.A;
+  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+  const int s = blockIdx.x, split = blockIdx.y;
+  if (tid == 0) {
+    for (int i = 0; i < kWarps * F::kRing; ++i) tc::mbar_init(&full[0][0] + i, 1);
+    abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  grid_wait_and_release();
+  const int len = attn_len(A, s), n_all = (len + kTile - 1) / kTile;
+  const int t0 = (int)((int64_t)n_all * split / A.splits), t1 = (int)((int64_t)n_all * (split + 1) / A.splits);
+  const int n_tiles = max(0, (t1 - t0 - warp + kWarps - 1) / kWarps);
+  if constexpr (!kBf16)
+    for (int i = tid; i < kR * D; i += kThreads)
+      qs[i] = i / D < A.n_rows ? static_cast<const float*>(A.q)[attn_row(A, s, i / D) * D + i % D] : 0.f;
+  __syncthreads();
+  const Ring<kBf16, D> R{&mk, &mv, tiles + warp * F::kRing * F::kTileBytes, full[warp], s, t0 + warp, 2 * n_tiles};
+  R.start(lane);
+  float* mrg = reinterpret_cast<float*>(tiles);  // [warp][row][kPitch], after the last tile
+  bool failed = false;
+  if constexpr (kBf16) few_warp_bf16<D>(P, R, s, len, n_tiles, lane, &abort_flag, mrg + warp * kFewRows * F::kPitch, failed);
+  else few_warp_fp32<D, kR>(P, R, s, len, n_tiles, lane, &abort_flag, qs, ps + warp * kR * 32, mrg + warp * kFewRows * F::kPitch, failed);
+  if (failed && lane == 0) tc::st_release(&abort_flag, 1);
+  __syncthreads();
+  // the warps' sums at one maximum
+  constexpr int kC = D / 32;
+  for (int r = warp; r < A.n_rows; r += kWarps) {
+    float top = -INFINITY, sum = 0.f, acc[kC] = {};
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) top = fmaxf(top, mrg[(w * kFewRows + r) * F::kPitch + D]);
+    const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      const float* from = mrg + (w * kFewRows + r) * F::kPitch;
+      const float f = exp2f(from[D] - base);
+      sum = fmaf(from[D + 1], f, sum);
+#pragma unroll
+      for (int c = 0; c < kC; ++c) acc[c] = fmaf(from[lane * kC + c], f, acc[c]);
+    }
+    if (abort_flag) sum = NAN;
+    const int64_t row = attn_row(A, s, r);
+    if (A.n_slots > 1) {
+      const int64_t at = (int64_t)(A.slot0 + split) * A.total_rows + row;
+      if (lane == 0) A.part_ml[at] = make_float2(top, sum);
+#pragma unroll
+      for (int c = 0; c < kC; c += 2) *reinterpret_cast<float2*>(A.part + at * D + lane * kC + c) = make_float2(acc[c], acc[c + 1]);
+      continue;
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    if (A.lse && lane == 0) A.lse[row] = sum == 0.f ? INFINITY : base + log2f(sum);
+#pragma unroll
+    for (int c = 0; c < kC; c += 2) {
+      if constexpr (kBf16)
+        *reinterpret_cast<__nv_bfloat162*>(static_cast<__nv_bfloat16*>(A.out) + row * D + lane * kC + c) = __floats2bfloat162_rn(acc[c] * inv, acc[c + 1] * inv);
+      else
+        *reinterpret_cast<float2*>(static_cast<float*>(A.out) + row * D + lane * kC + c) = make_float2(acc[c] * inv, acc[c + 1] * inv);
+    }
+  }
+}
+
+// Behind attn_few_kernel: the first `joins` CTAs join the splits, eight query rows each; the others turn 1024 logits per
+// query row into weights and add those of the scored rows up.
+constexpr int kEndThreads = 256, kEndKeys = 1024;
+template <bool kBf16, int D>
+__global__ void __launch_bounds__(kEndThreads) few_end_kernel(const __grid_constant__ FewArgs P, const ScoreArgs S, int joins, int chunks) {
+  __shared__ float lse[kFewRows];
+  const AttnRows& A = P.A;
+  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+  grid_wait_and_release();
+  if ((int)blockIdx.x < joins) {
+    const int64_t row = (int64_t)blockIdx.x * (kEndThreads / 32) + warp;
+    if (row < A.total_rows) join_splits<kBf16, D>(A, row, lane);
+    return;
+  }
+  const int s = ((int)blockIdx.x - joins) / chunks, k0 = ((int)blockIdx.x - joins) % chunks * kEndKeys;
+  const int len = attn_len(A, s);
+  if (k0 >= len) return;
+  if (warp < A.n_rows) {                         // (eight warps, at most eight rows)
+    const int64_t row = attn_row(A, s, warp);
+    float v = 0.f;
+    if (A.n_slots > 1) {
+      float top = -INFINITY, sum = 0.f;
+      for (int i = lane; i < A.n_slots; i += 32) top = fmaxf(top, A.part_ml[(int64_t)i * A.total_rows + row].x);
+      top = warp_max(top);
+      const float base = top == -INFINITY ? 0.f : top;
+      for (int i = lane; i < A.n_slots; i += 32) {
+        const float2 ml = A.part_ml[(int64_t)i * A.total_rows + row];
+        sum = fmaf(ml.y, exp2f(ml.x - base), sum);
+      }
+      sum = warp_sum(sum);
+      v = sum == 0.f ? INFINITY : base + log2f(sum);
+    } else {
+      v = A.lse[row];
+    }
+    if (warp % A.n_queries < A.n_queries - S.n_scored) v = INFINITY;      // not counted
+    if (lane == 0) lse[warp] = v;
+  }
+  __syncthreads();
+  const float* x = P.x + (int64_t)s * A.n_rows * P.pitch;
+  float sum[kEndKeys / kEndThreads] = {};
+  for (int r = 0; r < A.n_rows; ++r) {
+    const float off = lse[r];
+#pragma unroll
+    for (int j = 0; j < kEndKeys / kEndThreads; ++j) {
+      const int key = k0 + tid + j * kEndThreads;
+      if (key < len) sum[j] += exp2f(x[r * P.pitch + key] - off);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < kEndKeys / kEndThreads; ++j) {
+    const int key = k0 + tid + j * kEndThreads;
+    if (key < len) score_put(S, (int64_t)s * A.cap + key, sum[j]);
+  }
+}
+
+template <bool kBf16, int D, int kR>
+cudaError_t launch_few(const FewArgs& P, cudaStream_t st) {
+  using F = Few<kBf16, D>;
+  CUtensorMap mk, mv;
+  const AttnRows& A = P.A;
+  cudaError_t e = cache_map(&mk, A.K, kBf16, D, A.cap, A.n_streams, kTile);
+  if (e == cudaSuccess) e = cache_map(&mv, A.V, kBf16, D, A.cap, A.n_streams, kTile);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_few_kernel<kBf16, D, kR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)F::kSmem);
+  if (e != cudaSuccess) return e;
+  const PdlConfig pc(dim3(A.n_streams, A.splits), kThreads, F::kSmem, st);
+  return cudaLaunchKernelEx(&pc.cfg, attn_few_kernel<kBf16, D, kR>, P, mk, mv);
+}
+template <int D>
+cudaError_t launch_few_fp32(const FewArgs& P, cudaStream_t st) {
+  return P.A.n_rows <= 2 ? launch_few<false, D, 2>(P, st) : P.A.n_rows <= 4 ? launch_few<false, D, 4>(P, st) : launch_few<false, D, 8>(P, st);
+}
+template <bool kBf16, int D>
+cudaError_t launch_end(const FewArgs& P, const ScoreArgs& S, cudaStream_t st) {
+  const int joins = P.A.n_slots > 1 ? (P.A.total_rows + kEndThreads / 32 - 1) / (kEndThreads / 32) : 0;
+  const int chunks = (P.A.cap + kEndKeys - 1) / kEndKeys;
+  const PdlConfig pc(dim3((unsigned)(joins + chunks * P.A.n_streams)), kEndThreads, 0, st);
+  return cudaLaunchKernelEx(&pc.cfg, few_end_kernel<kBf16, D>, P, S, joins, chunks);
+}
+
+}  // namespace
+
+// Split factor of the kernels above: enough CTAs for several waves, so that streams of different lengths even out, and no
+// fewer than a tile for each warp of a CTA.
+int few_splits(int64_t streams, int cap) {
+  const int64_t want = (8 * kAttnSms + streams - 1) / streams, most = (cap + kWarps * kTile - 1) / (kWarps * kTile);
+  return (int)std::max<int64_t>(1, std::min<int64_t>({want, most, (int64_t)kAttnMaxSplits}));
+}
+
+int64_t few_pitch(int cap) { return ((int64_t)cap + 31) / 32 * 32; }
+
+// x: [n_streams, n_rows, few_pitch(cap)] where launch_few_end is to follow, else null.
+cudaError_t launch_attn_few(const AttnRows& A, float* x, int d, int is_bf16, cudaStream_t st) {
+  const FewArgs P{A, x, few_pitch(A.cap)};
+  if (is_bf16) return d == 128 ? launch_few<true, 128, 8>(P, st) : launch_few<true, 64, 8>(P, st);
+  return d == 128 ? launch_few_fp32<128>(P, st) : launch_few_fp32<64>(P, st);
+}
+
+// The scores, and the outputs where there are several splits.
+cudaError_t launch_few_end(const AttnRows& A, float* x, const ScoreArgs& S, int d, int is_bf16, cudaStream_t st) {
+  const FewArgs P{A, x, few_pitch(A.cap)};
+  if (is_bf16) return d == 128 ? launch_end<true, 128>(P, S, st) : launch_end<true, 64>(P, S, st);
+  return d == 128 ? launch_end<false, 128>(P, S, st) : launch_end<false, 64>(P, S, st);
+}
+
+}  // namespace bkv

@@ -29,15 +29,15 @@
 // tensor maps have the stream as a dimension of their own) are masked in the scores, and the V operand has the last valid
 // row in their place.  (Zeros there instead, by masks on the loaded registers or by clearing the tile's rows, made a launch
 // over 24 streams x 5000 rows 0.25 and 0.6 us slower; this takes less than 0.1 of 14.5.)
-#include <cuda.h>
-
 #include "decode_common.cuh"
+#include "tma_mma.cuh"
 
 namespace bkv {
 
 namespace {
 
 using namespace dec;
+using namespace mma;
 
 // Shape of a CTA: kGroups warp groups that take the CTA's tiles in turn, each warp of a group owning
 // kTB blocks of 16 tokens of a 64-token tile; two CTAs per SM.
@@ -70,11 +70,6 @@ struct DecodeMaps {
   CUtensorMap k, v;
 };
 
-__device__ inline void tma_load_3d(void* dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
-      ::"r"(smem_u32(dst)), "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z) : "memory");
-}
 // The same, and L2 may give its lines up first.
 __device__ inline void tma_load_3d_leaving(void* dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
   uint64_t policy;
@@ -86,33 +81,8 @@ __device__ inline void tma_load_3d_leaving(void* dst, const CUtensorMap* map, in
 __device__ inline void tma_prefetch_3d(const CUtensorMap* map, int x, int y, int z) {
   asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];" ::"l"(map), "r"(x), "r"(y), "r"(z) : "memory");
 }
-__device__ inline void ldsm_x4(uint32_t addr, uint32_t (&r)[4]) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
-}
-__device__ inline void ldsm_x4_trans(uint32_t addr, uint32_t (&r)[4]) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
-}
-__device__ inline void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-// Transpose of an 8 x 8 matrix of 16-bit elements held one row pair per thread (row lane / 4,
-// columns 2 (lane % 4) and the next): turns C-fragment rows into B-fragment columns.
-__device__ inline uint32_t movm_trans(uint32_t a) {
-  uint32_t d;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
-  return d;
-}
 static_assert(Dim<128>::kColWarps <= kWarps && 2 * Dim<128>::kColWarps <= 8,
               "a warp per 32 output columns; the scratch holds 8 floats of (max, sum) copies per partial row");
-__device__ inline uint32_t pack_bf16(float lo, float hi) {
-  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&v);
-}
 // Byte offset of (token row, 16-byte chunk of dims) inside a K or V tile: 64-dim boxes of
 // 64 rows x 128 bytes, chunk index XORed with (row % 8) by the 128-byte swizzle.
 __device__ inline uint32_t tile_off(int token, int chunk16) {   // chunk16 in [0, d / 8)
@@ -537,39 +507,10 @@ combine_kernel(Geom G, Arena A, __nv_bfloat16* __restrict__ out, float* __restri
   end.combine_head(0, part, 1, fac[warp], status);
 }
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
 // Tensor maps over K and V viewed as [n_streams, rows, d] bf16, boxes of 64 dims x 64 rows of one stream.
 cudaError_t encode_maps(DecodeMaps* tm, void* K, void* V, int d, int64_t rows, int n_streams) {
-  if (rows < 1 || rows >= ((int64_t)1 << 31)) return cudaErrorNotSupported;
-  struct Entry {
-    EncodeTiledFn fn = nullptr;
-    cudaError_t err = cudaSuccess;
-    Entry() {
-      void* p = nullptr;
-      cudaDriverEntryPointQueryResult qres;
-      err = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &qres);
-      if (err == cudaSuccess && (!p || qres != cudaDriverEntryPointSuccess)) err = cudaErrorNotSupported;
-      if (err == cudaSuccess) fn = reinterpret_cast<EncodeTiledFn>(p);
-    }
-  };
-  static const Entry entry;                 // the driver's encoder: looked up once
-  if (entry.err != cudaSuccess) return entry.err;
-  const cuuint64_t dims[3] = {(cuuint64_t)d, (cuuint64_t)rows, (cuuint64_t)n_streams};
-  const cuuint64_t strides[2] = {(cuuint64_t)d * 2, (cuuint64_t)d * 2 * rows};
-  const cuuint32_t box[3] = {64, (cuuint32_t)kTN, 1};
-  const cuuint32_t estr[3] = {1, 1, 1};
-  void* bases[2] = {K, V};
-  CUtensorMap* maps[2] = {&tm->k, &tm->v};
-  for (int i = 0; i < 2; ++i) {
-    CUresult r = entry.fn(maps[i], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, bases[i], dims, strides, box, estr,
-                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    if (r != CUDA_SUCCESS) return cudaErrorInvalidValue;
-  }
-  return cudaSuccess;
+  const cudaError_t e = cache_map(&tm->k, K, true, d, rows, n_streams, kTN);
+  return e != cudaSuccess ? e : cache_map(&tm->v, V, true, d, rows, n_streams, kTN);
 }
 
 template <int D>
