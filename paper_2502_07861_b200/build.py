@@ -10,8 +10,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libbalancekv.so")
 SOURCES = ["api.cu", "kernels_misc.cu", "kernels_walk_simt.cu", "kernels_walk_tc.cu", "kernels_ghat_tc.cu", "kernels_compact.cu",
            "kernels_decode.cu", "kernels_decode_mma.cu", "decode_static.cu", "kernels_bucket.cu", "kernels_anticorr.cu",
-           "cache_ops.cu", "kernels_attn_rows.cu", "kernels_attn_few.cu", "kernels_evict.cu"]
-HEADERS = ["common.cuh", "tcgen05.cuh", "decode_common.cuh", "attn_rows.cuh", "tma_mma.cuh", "sched.h", os.path.join("..", "..", "include", "balancekv.h")]
+           "cache_ops.cu", "kernels_attn_rows.cu", "kernels_attn_few.cu", "kernels_attn_tc.cu", "kernels_score_tc.cu", "kernels_evict.cu"]
+HEADERS = ["common.cuh", "tcgen05.cuh", "decode_common.cuh", "attn_rows.cuh", "attn_tc.cuh", "tma_mma.cuh", "sched.h", os.path.join("..", "..", "include", "balancekv.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC"]
 

@@ -97,6 +97,10 @@ int64_t few_pitch(int cap);
 cudaError_t launch_attn_few(const AttnRows& A, float* x, int d, int is_bf16, cudaStream_t st);
 cudaError_t launch_few_end(const AttnRows& A, float* x, const ScoreArgs& S, int d, int is_bf16, cudaStream_t st);
 
+int attn_tc_splits(const AttnRows& A);
+cudaError_t launch_attn_tc(const AttnRows& A, int d, cudaStream_t st);
+cudaError_t launch_score_tc(const AttnRows& A, const ScoreArgs& S, int d, cudaStream_t st);
+
 struct EvictArgs {
   const void *K, *V;
   const float* score;

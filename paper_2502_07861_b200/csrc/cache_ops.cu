@@ -64,7 +64,7 @@ int plan_scored(AttnRows& A, float*& x, Pieces& ws, int n_streams, int capacity,
   A.total_rows = (int)rows * n_streams;
   A.scale = (float)(1.4426950408889634 / std::sqrt((double)head_dim));
   const bool few = rows <= kFewRows;
-  A.n_slots = A.splits = few ? few_splits(n_streams, capacity) : simt_splits((rows + 63) / 64 * n_streams, capacity);
+  A.n_slots = A.splits = few ? few_splits(n_streams, capacity) : dtype ? attn_tc_splits(A) : simt_splits((rows + 63) / 64 * n_streams, capacity);
   take_parts(A, ws, head_dim);
   if (n_scored) A.lse = ws.take<float>(A.total_rows);
   x = n_scored && few ? ws.take<float>(A.total_rows * few_pitch(capacity)) : nullptr;
@@ -87,7 +87,7 @@ int plan_prefix(AttnRows& P, AttnRows& A, Pieces& ws, int prefix_len, int capaci
   P.n_rows = n_seqs * group;
   P.q_stream = P.q_inner = group;
   P.q_outer = n_kv_heads * group;
-  P.splits = simt_splits((int64_t)(P.n_rows + 63) / 64 * n_kv_heads, prefix_len);
+  P.splits = dtype ? attn_tc_splits(P) : simt_splits((int64_t)(P.n_rows + 63) / 64 * n_kv_heads, prefix_len);
   A.n_streams = (int)streams;                  // a sequence's own rows
   A.lens_div = n_kv_heads;
   A.cap = capacity;
@@ -157,9 +157,9 @@ extern "C" int balancekv_attn_scored(const void* K, const void* V, const int32_t
     if (e == cudaSuccess && n_scored) e = launch_few_end(A, x, S, head_dim, dtype, st);
     else if (e == cudaSuccess && A.n_slots > 1) e = launch_attn_combine(A, head_dim, dtype, st);
   } else {
-    e = launch_attn_simt(A, head_dim, dtype, st);
+    e = dtype ? launch_attn_tc(A, head_dim, st) : launch_attn_simt(A, head_dim, dtype, st);
     if (e == cudaSuccess && A.n_slots > 1) e = launch_attn_combine(A, head_dim, dtype, st);
-    if (e == cudaSuccess && n_scored) e = launch_score_simt(A, S, head_dim, dtype, st);
+    if (e == cudaSuccess && n_scored) e = dtype ? launch_score_tc(A, S, head_dim, st) : launch_score_simt(A, S, head_dim, dtype, st);
   }
   return report("balancekv_attn_scored", e);
 }
@@ -195,7 +195,7 @@ extern "C" int balancekv_decode_attn_prefix(const void* K_prefix, const void* V_
   P.q = A.q = q;
   P.out = A.out = out;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  cudaError_t e = launch_attn_simt(P, head_dim, dtype, st);
+  cudaError_t e = dtype ? launch_attn_tc(P, head_dim, st) : launch_attn_simt(P, head_dim, dtype, st);
   if (e == cudaSuccess && A.splits) e = launch_attn_few(A, nullptr, head_dim, dtype, st);
   if (e == cudaSuccess && P.n_slots > 1) e = launch_attn_combine(P, head_dim, dtype, st);
   return report("balancekv_decode_attn_prefix", e);

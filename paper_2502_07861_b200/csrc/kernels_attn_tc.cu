@@ -1,0 +1,425 @@
+// Attention of many query rows over a caller-held cache in bf16 on the 5th-generation tensor cores.
+//
+//   x_{r,i} = <q_r, k_i> log2(e) / sqrt d + log2 w_i,   out_r = sum_i 2^(x_{r,i} - m_r) v_i / sum_i 2^(x_{r,i} - m_r)
+//
+// A CTA takes two tiles of up to 128 query rows of a stream and walks its share of the keys in tiles of 128.  Per tile of logits:
+// S = Q K^T (tcgen05.mma, both operands in shared memory) into TMEM; a warpgroup, a thread per query row, turns S into weights and
+// writes them over S as bf16; O += P V (P from TMEM).  Two tiles take turns, so that the tensor core multiplies for one while the
+// other's exponentials are formed: per pair of tiles the products take 2048 cycles (d = 128), and so would 32768 exponentials of the
+// special-function unit; a share of them is therefore formed by FMAs.
+// The maximum m_r is the one seen when it last grew by more than 8: weights then stay below 2^8 and O is brought to a new maximum
+// only that often (usually in the first tiles).  Sums and maxima are fp32; the weights are rounded to bf16 for the second product,
+// their sum is not.
+//
+// Warps: 0-3 and 4-7 the rows of the two tiles, 8 asks for Q, K and V tiles (TMA, 128-byte swizzle, a ring), 9 issues the MMAs.
+// Rows of V (weighted: of K too) that no query may see -- behind the last row in use, of weight zero -- are cleared in shared memory
+// by warp 9 before it multiplies with them, since zero times what they hold need not be zero.
+// Every wait is bounded; one that gives up makes the results NaN.
+#include <algorithm>
+
+#include "attn_tc.cuh"
+
+namespace bkv {
+
+namespace {
+
+using namespace tc;
+using namespace mma;
+
+constexpr int kThreads = 384;
+// Registers of a thread at launch, and what the warps go on with: 8 x 208 + 4 x 80 <= 12 x 168.
+constexpr int kRegs = 168, kRegsRows = 208, kRegsOther = 80;
+static_assert(8 * kRegsRows + 4 * kRegsOther <= 12 * kRegs && kThreads * kRegs <= 65536, "a register split beyond the launch's waits forever");
+constexpr float kGrow = 8.f;                     // the maximum follows when it would grow by more
+
+template <int D>
+struct Shape {
+  static constexpr uint32_t kBox = 128 * 128;                          // bytes: 64 dims x 128 rows
+  static constexpr uint32_t kTile = (D / 64) * kBox;
+  static constexpr int kRing = D == 128 ? 5 : 8;                       // K and V tiles in turn
+  // Tiles of log weights: tile j takes the place of tile j - kBias, which has been read: its entry of V (d = 64: of K) has been freed.
+  static constexpr int kBias = D == 128 ? 3 : 8;
+  static constexpr size_t kSmem = 1024 + (2 + kRing) * (size_t)kTile;
+};
+
+struct TcArgs {
+  AttnRows A;
+  int32_t rows_per_tile;       // query rows of a tile: 128, or the largest multiple of the group that fits
+  int32_t q_outer_rows;        // rows of the query box's outer dimension per tile (0: the query rows are contiguous)
+  int32_t blocks;              // of two tiles of query rows, per stream
+};
+
+// kWeighted: every query sees every row in use, with weights.
+template <int D, bool kWeighted>
+__global__ void __maxnreg__(kRegs)
+attn_tc_kernel(const __grid_constant__ TcArgs P, const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv) {
+  using Sh = Shape<D>;
+  constexpr int kRing = Sh::kRing;
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ uint64_t q_full, kv_full[kRing], kv_empty[kRing], s_full[2], p_full[2][2], o_done[2], bias_full[Sh::kBias], drained;
+  __shared__ uint32_t tmem_s;
+  __shared__ int abort_flag;
+  __shared__ __align__(16) float bias[kWeighted ? Sh::kBias : 1][kTcKeys];
+  const AttnRows& A = P.A;
+  unsigned char* sm = smem_raw + (-smem_u32(smem_raw) & 1023u);
+  unsigned char* ring = sm + 2 * Sh::kTile;
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid / 32, 0), lane = tid % 32;
+  if (tid == 0) {
+    mbar_init(&q_full, 1);
+    mbar_init(&drained, 1);
+    for (int i = 0; i < kRing; ++i) { mbar_init(kv_full + i, 1); mbar_init(kv_empty + i, 1); }
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(s_full + t, 1);
+      mbar_init(o_done + t, 1);
+      mbar_init(&p_full[t][0], 128);
+      mbar_init(&p_full[t][1], 128);
+    }
+    for (int i = 0; i < Sh::kBias; ++i) mbar_init(bias_full + i, 32);
+    abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 9) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_s)), "r"(512u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  grid_wait_and_release();
+  // the last query rows, which see the most, first
+  const int s = blockIdx.x % A.n_streams, block = P.blocks - 1 - blockIdx.x / A.n_streams, split = blockIdx.y;
+  const int len = attn_len(A, s);
+  // Of either tile: the tiles of keys that some row sees, and the first of them that not every row sees whole.
+  int n_t[2], whole[2];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const int r0 = (2 * block + t) * P.rows_per_tile, r1 = min(r0 + P.rows_per_tile, A.n_rows) - 1;
+    if (r0 >= A.n_rows) { n_t[t] = 0; whole[t] = 0; continue; }
+    const bool wraps = r0 / A.n_queries != r1 / A.n_queries;
+    n_t[t] = ((wraps ? len : attn_limit(A, len, r1)) + kTcKeys - 1) / kTcKeys;
+    whole[t] = (wraps ? attn_limit(A, len, 0) : attn_limit(A, len, r0)) / kTcKeys;
+  }
+  const int all = max(n_t[0], n_t[1]);
+  const int j0 = (int)((int64_t)all * split / A.splits), j1 = (int)((int64_t)all * (split + 1) / A.splits);
+#pragma unroll
+  for (int t = 0; t < 2; ++t) n_t[t] = max(0, min(n_t[t], j1) - j0);
+  const int n = max(n_t[0], n_t[1]);             // tiles of keys that this CTA loads: j0 .. j0 + n - 1
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_s, 0);
+
+  if (warp >= 8) {
+    regs_down<kRegsOther>();
+    if (warp == 8) {
+      bool ok = true;
+      const int q_tiles = (n_t[0] > 0) + (n_t[1] > 0);
+      if (lane == 0 && n > 0) {
+        mbar_expect_tx(&q_full, (uint32_t)q_tiles * P.rows_per_tile * 2 * D);
+        for (int t = 0; t < 2; ++t) {
+          if (n_t[t] == 0) continue;
+          const int r0 = (2 * block + t) * P.rows_per_tile;
+          for (int b = 0; b < D / 64; ++b) {
+            if (P.q_outer_rows) tma_load_3d(sm + t * Sh::kTile + b * Sh::kBox, &mq, 64 * b, s * A.q_stream, r0 / A.q_inner, &q_full);
+            else tma_load_3d(sm + t * Sh::kTile + b * Sh::kBox, &mq, 64 * b, s * A.q_stream + r0, 0, &q_full);
+          }
+        }
+      }
+      int e = 0;
+      for (; e < 2 * n; ++e) {
+        const int slot = e % kRing, key0 = (j0 + e / 2) * kTcKeys;
+        if (e >= kRing) ok = wait_bar(kv_empty + slot, (uint32_t)(e / kRing - 1) & 1u, &abort_flag);
+        if (!__all_sync(0xffffffffu, ok)) break;
+        if (lane == 0) {
+          mbar_expect_tx(kv_full + slot, Sh::kTile);
+          for (int b = 0; b < D / 64; ++b) tma_load_3d(ring + slot * Sh::kTile + b * Sh::kBox, e & 1 ? &mv : &mk, 64 * b, key0, s, kv_full + slot);
+        }
+        if (kWeighted && !(e & 1)) {             // the tile of log weights; its place was last read before the ring's entry was freed
+          float* to = bias[(e / 2) % Sh::kBias];
+#pragma unroll
+          for (int i = 0; i < kTcKeys / 32; ++i) {
+            const int key = key0 + lane + 32 * i;
+            to[lane + 32 * i] = key < len ? (A.w ? log2f(A.w[(int64_t)s * A.cap + key]) : 0.f) : -INFINITY;
+          }
+          mbar_arrive(bias_full + (e / 2) % Sh::kBias);
+        }
+        __syncwarp();
+      }
+      if (e < 2 * n && lane == 0) {              // gave up: the copies in flight, within limits
+        const long long t0 = clock64();
+        for (int i = max(0, e - kRing); i < e; ++i)
+          while (!mbar_try_wait(kv_full + i % kRing, (uint32_t)(i / kRing) & 1u) && clock64() - t0 < kWaitCycles) {}
+      }
+    } else if (warp == 9 && n > 0) {
+      constexpr uint32_t kInstrPv = kInstrBf16<D> | kOuterB;
+      bool ok = true;
+      auto wait = [&](uint64_t* bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, wait_bar(bar, parity, &abort_flag)); };
+      auto wait_kv = [&](int e) { wait(kv_full + e % kRing, (uint32_t)(e / kRing) & 1u); };
+      // Rows of entry e that nobody may see become zeros.
+      auto clear = [&](int e) {
+        const int key0 = (j0 + e / 2) * kTcKeys;
+        if (!kWeighted && ((e & 1) == 0 || key0 + kTcKeys <= len)) return;
+        bool any = key0 + kTcKeys > len;
+        if constexpr (kWeighted) {
+          wait(bias_full + (e / 2) % Sh::kBias, (uint32_t)(e / 2 / Sh::kBias) & 1u);
+          const float4 b = *reinterpret_cast<const float4*>(bias[(e / 2) % Sh::kBias] + 4 * lane);
+          any = __any_sync(0xffffffffu, b.x == -INFINITY || b.y == -INFINITY || b.z == -INFINITY || b.w == -INFINITY);
+        }
+        if (!any || !ok) return;
+        unsigned char* tile = ring + e % kRing * Sh::kTile;
+        for (int r = 0; r < kTcKeys; ++r) {
+          bool gone = key0 + r >= len;
+          if constexpr (kWeighted) gone = bias[(e / 2) % Sh::kBias][r] == -INFINITY;
+          if (gone && lane < D / 8) *reinterpret_cast<uint4*>(tile + (lane / 8) * Sh::kBox + r * 128 + (lane % 8) * 16) = make_uint4(0, 0, 0, 0);
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+      };
+      auto qk = [&](int t, int j) {
+        if (elect_one()) {
+          const uint32_t a = umma_desc_lo(smem_u32(sm + t * Sh::kTile)), b = umma_desc_lo(smem_u32(ring + (2 * j) % kRing * Sh::kTile));
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k) {
+            const uint32_t at = (uint32_t)(k / 4) * (Sh::kBox >> 4) + 2 * (k % 4);
+            if (k == 0) umma_bf16<0>(tmem + 128 * t, a + at, b + at);
+            else umma_bf16<1>(tmem + 128 * t, a + at, b + at);
+          }
+          umma_commit(s_full + t);
+          if (t == (j < n_t[1])) umma_commit(kv_empty + (2 * j) % kRing);
+        }
+        __syncwarp();
+      };
+      wait(&q_full, 0);
+      wait_kv(0);
+      if (kWeighted) clear(0);
+      tc_fence_after();
+      for (int t = 0; t < 2; ++t)
+        if (ok && n_t[t] > 0) qk(t, 0);
+      for (int j = 0; j < n && ok; ++j) {
+        for (int t = 0; t < 2 && ok; ++t) {
+          if (j >= n_t[t]) continue;
+          const int last_t = j < n_t[1];
+          if (t == 0 || n_t[0] <= j) {
+            wait_kv(2 * j + 1);
+            clear(2 * j + 1);
+          }
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            wait(&p_full[t][h], (uint32_t)j & 1u);
+            tc_fence_after();
+            if (ok && elect_one()) {
+              const uint32_t v = umma_desc_lo_outer(smem_u32(ring + (2 * j + 1) % kRing * Sh::kTile), Sh::kBox);
+#pragma unroll
+              for (int k = 4 * h; k < 4 * h + 4; ++k)
+                umma_ts<kInstrPv>(tmem + 256 + D * t, tmem + 128 * t + 8 * k, v + 128 * k, j > 0 || k > 0);
+              if (h == 1) {
+                umma_commit(o_done + t);
+                if (t == last_t) umma_commit(kv_empty + (2 * j + 1) % kRing);
+              }
+            }
+            __syncwarp();
+          }
+          if (j + 1 < n_t[t] && ok) {
+            if (t == 0 || n_t[0] <= j + 1) {
+              wait_kv(2 * j + 2);
+              if (kWeighted) clear(2 * j + 2);
+            }
+            tc_fence_after();
+            if (ok) qk(t, j + 1);
+          }
+        }
+      }
+      if (!ok) {                                 // gave up: the products in flight, within limits
+        if (elect_one()) umma_commit(&drained);
+        st_release(&abort_flag, 1);
+        const long long t0 = clock64();
+        while (!mbar_try_wait(&drained, 0) && clock64() - t0 < kWaitCycles) {}
+      }
+    }
+  } else {
+    regs_up<kRegsRows>();
+    const int t = warp / 4;
+    const int r = (2 * block + t) * P.rows_per_tile + 32 * (warp % 4) + lane;
+    const bool valid = 32 * (warp % 4) + lane < P.rows_per_tile && r < A.n_rows;
+    const int limit = valid ? attn_limit(A, len, r) : 0;
+    const uint32_t S = tmem + ((uint32_t)(32 * (warp % 4)) << 16) + 128 * t, O = tmem + ((uint32_t)(32 * (warp % 4)) << 16) + 256 + D * t;
+    const int mine = n_t[t];
+    const float2 scale2 = make_float2(A.scale, A.scale);
+    float m = -INFINITY;
+    float2 l2 = make_float2(0.f, 0.f);
+    bool ok = true;
+    for (int j = 0; j < mine; ++j) {
+      ok = __all_sync(0xffffffffu, wait_bar(s_full + t, (uint32_t)j & 1u, &abort_flag));
+      if (ok && kWeighted) ok = __all_sync(0xffffffffu, wait_bar(bias_full + j % Sh::kBias, (uint32_t)(j / Sh::kBias) & 1u, &abort_flag));
+      if (!ok) break;
+      tc_fence_after();
+      float x[4][32];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tmem_ld32(S + 32 * c, x[c]);
+      tmem_ld_wait();
+      const bool masked = !kWeighted && j0 + j >= whole[t];
+      if constexpr (kWeighted) {
+        const float4* b4 = reinterpret_cast<const float4*>(bias[j % Sh::kBias]);
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int i = 0; i < 32; i += 4) {
+            const float4 b = b4[(32 * c + i) / 4];
+            const float2 lo = __ffma2_rn(make_float2(x[c][i], x[c][i + 1]), scale2, make_float2(b.x, b.y));
+            const float2 hi = __ffma2_rn(make_float2(x[c][i + 2], x[c][i + 3]), scale2, make_float2(b.z, b.w));
+            x[c][i] = lo.x; x[c][i + 1] = lo.y; x[c][i + 2] = hi.x; x[c][i + 3] = hi.y;
+          }
+      }
+      if (masked) {
+        const int sees = limit - (j0 + j) * kTcKeys;
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int i = 0; i < 32; ++i) x[c][i] = 32 * c + i < sees ? x[c][i] : -INFINITY;
+      }
+      float top[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        top[c] = fmaxf(x[c][0], x[c][1]);
+#pragma unroll
+        for (int i = 2; i < 32; ++i) top[c] = fmaxf(top[c], x[c][i]);
+      }
+      float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+      if (!kWeighted) mx *= A.scale;
+      const bool grow = mx > m + kGrow;
+      if (__any_sync(0xffffffffu, grow)) {
+        const float f = grow ? ex2(m - mx) : 1.f;
+        if (grow) m = mx;
+        l2.x *= f;
+        l2.y *= f;
+        if (j > 0) {                             // O at the new maximum, once the products before are in it
+          ok = __all_sync(0xffffffffu, wait_bar(o_done + t, (uint32_t)(j - 1) & 1u, &abort_flag));
+          if (!ok) break;
+          tc_fence_after();
+#pragma unroll 1
+          for (int c = 0; c < D; c += 16) {
+            float o[16];
+            tmem_ld16(O + c, o);
+            tmem_ld_wait();
+            uint32_t w[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(o[i] * f);
+            tmem_st16(O + c, w);
+          }
+        }
+      }
+      const float base = m == -INFINITY ? 0.f : -m;
+      const float2 base2 = make_float2(base, base);
+      const float2 one2 = kWeighted ? make_float2(1.f, 1.f) : scale2;
+      auto weights = [&](auto all_mufu) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          uint32_t w[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const float2 y = __ffma2_rn(make_float2(x[c][2 * i], x[c][2 * i + 1]), one2, base2);
+            float2 p;
+            if (!decltype(all_mufu)::value && i % 4 == 3) p = exp2_fma(y);
+            else p = make_float2(ex2(y.x), ex2(y.y));
+            l2 = __fadd2_rn(l2, p);
+            w[i] = pack_bf16(p.x, p.y);
+          }
+          tmem_st16(S + 16 * c, w);
+          if (c & 1) {
+            tmem_st_wait();
+            tc_fence_before();
+            mbar_arrive(&p_full[t][c / 2]);
+          }
+        }
+      };
+      if (masked) weights(std::true_type{});     // (what is masked has weight zero, which exp2_fma does not give)
+      else weights(std::false_type{});
+    }
+    float l = l2.x + l2.y;
+    if (mine > 0 && ok) {
+      ok = __all_sync(0xffffffffu, wait_bar(o_done + t, (uint32_t)(mine - 1) & 1u, &abort_flag));
+      tc_fence_after();
+    }
+    if (!ok) l = NAN;
+    const int64_t row = valid ? attn_row(A, s, r) : 0;
+    const bool parts = A.n_slots > 1;
+    const float inv = parts ? 1.f : l == 0.f ? 0.f : 1.f / l;
+    const int64_t at = (int64_t)(A.slot0 + split) * A.total_rows + row;
+    if (valid && parts) A.part_ml[at] = make_float2(m, l);
+    if (valid && !parts && A.lse) A.lse[row] = l == 0.f ? INFINITY : m + log2f(l);
+#pragma unroll
+    for (int c = 0; c < D; c += 32) {
+      float o[32];
+      if (mine > 0) {
+        tmem_ld32(O + c, o);
+        tmem_ld_wait();
+      }
+#pragma unroll
+      for (int i = 0; i < 32; ++i) o[i] = mine > 0 && l != 0.f ? o[i] * inv : 0.f;
+      if (!valid) {
+      } else if (parts) {
+        float4* to = reinterpret_cast<float4*>(A.part + at * D + c);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) to[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+      } else {
+        uint4* to = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(A.out) + row * D + c);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          to[i] = make_uint4(pack_bf16(o[8 * i], o[8 * i + 1]), pack_bf16(o[8 * i + 2], o[8 * i + 3]), pack_bf16(o[8 * i + 4], o[8 * i + 5]), pack_bf16(o[8 * i + 6], o[8 * i + 7]));
+      }
+      __syncwarp();
+    }
+    tc_fence_before();
+  }
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+}
+
+// Query rows of a stream: contiguous (box 64 dims x 128 rows), or `inner` of each of an outer dimension's.
+cudaError_t query_map(CUtensorMap* map, const AttnRows& A, int d, int outer_rows) {
+  EncodeTiledFn encode = nullptr;
+  const cudaError_t e = tensor_map_encoder(&encode);
+  if (e != cudaSuccess) return e;
+  const cuuint64_t inner = outer_rows ? (cuuint64_t)A.q_outer : (cuuint64_t)A.total_rows;
+  const cuuint64_t dims[3] = {(cuuint64_t)d, inner, (cuuint64_t)A.total_rows / inner};
+  const cuuint64_t strides[2] = {(cuuint64_t)d * 2, (cuuint64_t)d * 2 * inner};
+  const cuuint32_t box[3] = {64, outer_rows ? (cuuint32_t)A.q_inner : 128u, outer_rows ? (cuuint32_t)outer_rows : 1u};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(A.q), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+template <int D, bool kWeighted>
+cudaError_t launch(const TcArgs& P, cudaStream_t st) {
+  const AttnRows& A = P.A;
+  CUtensorMap mq, mk, mv;
+  cudaError_t e = query_map(&mq, A, D, P.q_outer_rows);
+  if (e == cudaSuccess) e = cache_map(&mk, A.K, true, D, A.cap, A.n_streams, kTcKeys);
+  if (e == cudaSuccess) e = cache_map(&mv, A.V, true, D, A.cap, A.n_streams, kTcKeys);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_tc_kernel<D, kWeighted>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Shape<D>::kSmem);
+  if (e != cudaSuccess) return e;
+  const PdlConfig pc(dim3((unsigned)P.blocks * A.n_streams, A.splits), kThreads, Shape<D>::kSmem, st);
+  return cudaLaunchKernelEx(&pc.cfg, attn_tc_kernel<D, kWeighted>, P, mq, mk, mv);
+}
+
+// Rows of a tile: with an outer dimension whole groups of it.
+int rows_per_tile(const AttnRows& A) { return A.q_outer ? 128 / A.q_inner * A.q_inner : 128; }
+
+}  // namespace
+
+// CTAs that share the keys of a block of query rows: as many as make one wave (a CTA has an SM to itself), with two tiles of keys each
+// at least.
+int attn_tc_splits(const AttnRows& A) {
+  const int64_t blocks = (int64_t)(A.n_rows + 2 * rows_per_tile(A) - 1) / (2 * rows_per_tile(A)) * A.n_streams;
+  const int64_t tiles = (A.cap + kTcKeys - 1) / kTcKeys, want = kAttnSms / blocks;
+  return (int)std::max<int64_t>(1, std::min<int64_t>({want, tiles / 2, (int64_t)kAttnMaxSplits}));
+}
+
+cudaError_t launch_attn_tc(const AttnRows& A, int d, cudaStream_t st) {
+  TcArgs P{A, rows_per_tile(A), A.q_outer ? 128 / A.q_inner : 0, 0};
+  P.blocks = (A.n_rows + 2 * P.rows_per_tile - 1) / (2 * P.rows_per_tile);
+  if (A.w) return d == 128 ? launch<128, true>(P, st) : launch<64, true>(P, st);
+  return d == 128 ? launch<128, false>(P, st) : launch<64, false>(P, st);
+}
+
+}  // namespace bkv
