@@ -7,6 +7,7 @@ library or a failing CUDA call raises.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -454,67 +455,58 @@ def decode_attn_static_status(stream=None):
     return v.value
 
 
-def _on_device(what, device, **tensors):
-    """Every tensor given is a contiguous CUDA tensor of the current device, whose stream the call runs on."""
+def _expect(what, device, name, t, dtype, shape):
+    """``t`` (or None) is a contiguous tensor of this dtype and shape on CUDA device number ``device``."""
+    if t is None or (t.dtype is dtype and t.shape == shape and t.get_device() == device and t.is_contiguous()):
+        return
+    if t.dtype is not dtype or t.shape != shape:
+        raise ValueError(f"{what}: {name}: expected dtype {dtype} and shape {tuple(shape)}, got {t.dtype} and {tuple(t.shape)}")
+    raise ValueError(f"{what}: {name}: expected a contiguous tensor on CUDA device {device}")
+
+
+def _on_current(what, device, t):
+    """The call runs on a stream of the current CUDA device, which has to be the tensors'."""
     import torch
 
-    if device.type != "cuda" or device.index != torch._C._cuda_getDevice():
-        raise ValueError(f"{what}: the tensors are on {device}, not on the current CUDA device")
-    for name, t in tensors.items():
-        if t is not None and (t.device != device or not t.is_contiguous()):
-            raise ValueError(f"{what}: {name}: expected a contiguous tensor on {device}")
-
-
-def _typed(what, dtype, **tensors):
-    for name, t in tensors.items():
-        if t is not None and t.dtype != dtype:
-            raise ValueError(f"{what}: {name}: expected dtype {dtype}, got {t.dtype}")
-
-
-def _shaped(what, **tensors):
-    for name, (t, shape) in tensors.items():
-        if t is not None and tuple(t.shape) != tuple(shape):
-            raise ValueError(f"{what}: {name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    if device < 0 or device != torch._C._cuda_getDevice():
+        raise ValueError(f"{what}: the tensors are on {t.device}, not on the current CUDA device")
 
 
 def _dtype_code(what, dtype):
     import torch
 
-    if dtype not in (torch.bfloat16, torch.float32):
-        raise ValueError(f"{what}: dtype {dtype} is neither torch.bfloat16 nor torch.float32")
-    return 1 if dtype == torch.bfloat16 else 0
+    if dtype is torch.bfloat16:
+        return 1
+    if dtype is torch.float32:
+        return 0
+    raise ValueError(f"{what}: dtype {dtype} is neither torch.bfloat16 nor torch.float32")
 
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-class _AllocateOn:
+def _on_stream(stream):
     """Tensors made inside belong to the stream of the call, so that their memory is not handed on while it still runs."""
-
-    def __init__(self, stream):
-        import torch
-
-        if isinstance(stream, int):
-            stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
-        self._on = None if stream is None else torch.cuda.stream(stream)
-
-    def __enter__(self):
-        if self._on is not None:
-            self._on.__enter__()
-
-    def __exit__(self, *exc):
-        if self._on is not None:
-            self._on.__exit__(*exc)
-
-
-def _workspace(what, device, *args):
-    """A workspace of the bytes that ``what``_workspace asks for."""
     import torch
 
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+    return torch.cuda.stream(stream)
+
+
+@functools.lru_cache(maxsize=1024)
+def _workspace_bytes(name, *sizes):
+    """What ``name``_workspace asks for: a function of the sizes alone."""
     size = C.c_size_t(0)
-    _check(getattr(load(), what + "_workspace")(*args, C.byref(size)), what + "_workspace")
-    return torch.empty(size.value, dtype=torch.uint8, device=device) if size.value else None, size.value
+    _check(getattr(load(), name + "_workspace")(*sizes, C.byref(size)), name + "_workspace")
+    return size.value
+
+
+def _workspace(device, size):
+    import torch
+
+    return torch.empty(size, dtype=torch.uint8, device=device) if size else None
 
 
 def attn_scored(K, V, q, lens=None, score=None, score_out=None, n_scored=None, decay=1.0, out=None, stream=None):
@@ -526,27 +518,32 @@ def attn_scored(K, V, q, lens=None, score=None, score_out=None, n_scored=None, d
     new tensor of zeros.  Returns (out, score_out); with n_scored = 0 the second is ``score_out`` as it was."""
     import torch
 
+    if stream is not None:
+        with _on_stream(stream):
+            return attn_scored(K, V, q, lens, score, score_out, n_scored, decay, out)
     what = "balancekv_attn_scored"
     if K.dim() != 3 or q.dim() not in (3, 4):
         raise ValueError(f"{what}: expected K [n_streams, capacity, d] and q [n_streams, group, (n_queries,) d]")
     (S, cap, d), group, m = K.shape, q.shape[1], q.shape[2] if q.dim() == 4 else 1
-    code = _dtype_code(what, K.dtype)
+    dtype, code, device = K.dtype, _dtype_code(what, K.dtype), K.get_device()
     if n_scored is None:
         n_scored = m
-    _typed(what, K.dtype, V=V, q=q, out=out)
-    _typed(what, torch.float32, score=score, score_out=score_out)
-    _typed(what, torch.int32, lens=lens)
-    _shaped(what, V=(V, (S, cap, d)), q=(q, (S, group, m, d) if q.dim() == 4 else (S, group, d)), lens=(lens, (S,)), score=(score, (S, cap)),
-            score_out=(score_out, (S, cap)), out=(out, q.shape))
-    _on_device(what, K.device, K=K, V=V, q=q, lens=lens, score=score, score_out=score_out, out=out)
-    with _AllocateOn(stream):
-        if out is None:
-            out = torch.empty_like(q)
-        if score_out is None and n_scored:
-            score_out = torch.zeros(S, cap, device=K.device) if score is None else score
-        ws, size = _workspace(what, K.device, S, cap, m, group, d, code, n_scored)
-        _check(load().balancekv_attn_scored(K.data_ptr(), V.data_ptr(), _ptr(lens), S, cap, q.data_ptr(), out.data_ptr(), m, group, d, code,
-                                            _ptr(score), _ptr(score_out), n_scored, decay, _ptr(ws), size, _stream_ptr(stream)), what)
+    _expect(what, device, "K", K, dtype, (S, cap, d))
+    _expect(what, device, "V", V, dtype, (S, cap, d))
+    _expect(what, device, "q", q, dtype, (S, group, m, d) if q.dim() == 4 else (S, group, d))
+    _expect(what, device, "out", out, dtype, q.shape)
+    _expect(what, device, "lens", lens, torch.int32, (S,))
+    _expect(what, device, "score", score, torch.float32, (S, cap))
+    _expect(what, device, "score_out", score_out, torch.float32, (S, cap))
+    _on_current(what, device, K)
+    if out is None:
+        out = torch.empty_like(q)
+    if score_out is None and n_scored:
+        score_out = torch.zeros(S, cap, device=K.device) if score is None else score
+    size = _workspace_bytes(what, S, cap, m, group, d, code, n_scored)
+    ws = _workspace(K.device, size)
+    _check(load().balancekv_attn_scored(K.data_ptr(), V.data_ptr(), _ptr(lens), S, cap, q.data_ptr(), out.data_ptr(), m, group, d, code,
+                                        _ptr(score), _ptr(score_out), n_scored, decay, _ptr(ws), size, _stream_ptr(None)), what)
     return out, score_out
 
 
@@ -554,22 +551,32 @@ def cache_evict(K, V, score, n_keep, lens=None, pos=None, n_first=0, n_recent=0,
     """Keep the ``n_keep`` rows of every stream that received the most weight, and the first and newest positions (see balancekv.h).
 
     K, V: CUDA tensors [n_streams, capacity, d]; score: float32, pos (None: the rows' numbers): int32, both [n_streams, capacity];
-    lens: int32 [n_streams] (None: all rows are in use).  ``out``: a dict of "k", "v", "score", "pos" and "lens" to fill, by default
-    new tensors of min(n_keep, capacity) rows whose unused ones are zero; with ``in_place`` the cache itself, of which only the rows that fill a hole move
-    (``pos`` and ``lens`` are updated if given, ``lens`` is made if not).  Returns that dict."""
+    lens: int32 [n_streams] (None: all rows are in use).  ``out``: a dict of "k", "v", "score" and, if they are wanted, "pos" and "lens" to
+    fill, by default new tensors of min(n_keep, capacity) rows whose unused ones are zero; with ``in_place`` the cache itself, of which only
+    the rows that fill a hole move (``pos`` and ``lens`` are updated if given, ``lens`` is made if not).  Returns that dict."""
     import torch
 
+    if stream is not None:
+        with _on_stream(stream):
+            return cache_evict(K, V, score, n_keep, lens, pos, n_first, n_recent, out, in_place)
     what = "balancekv_cache_evict"
     if K.dim() != 3:
         raise ValueError(f"{what}: expected K [n_streams, capacity, d]")
     S, cap, d = K.shape
-    code = _dtype_code(what, K.dtype)
-    if in_place and out is not None:
-        raise ValueError(f"{what}: either out or in_place")
-    with _AllocateOn(stream):
-        if in_place:
-            out = {"k": K, "v": V, "score": score, "pos": pos, "lens": torch.empty(S, dtype=torch.int32, device=K.device) if lens is None else lens}
-        elif out is None:
+    dtype, code, device = K.dtype, _dtype_code(what, K.dtype), K.get_device()
+    _expect(what, device, "K", K, dtype, (S, cap, d))
+    _expect(what, device, "V", V, dtype, (S, cap, d))
+    _expect(what, device, "score", score, torch.float32, (S, cap))
+    _expect(what, device, "pos", pos, torch.int32, (S, cap))
+    _expect(what, device, "lens", lens, torch.int32, (S,))
+    _on_current(what, device, K)
+    if in_place:
+        if out is not None:
+            raise ValueError(f"{what}: either out or in_place")
+        out = {"k": K, "v": V, "score": score, "pos": pos, "lens": torch.empty(S, dtype=torch.int32, device=K.device) if lens is None else lens}
+        Ko, Vo, so, po, lo, rows = K, V, score, pos, out["lens"], cap
+    else:
+        if out is None:
             rows = min(n_keep, cap)
             if rows < 1:
                 raise ValueError(f"{what}: n_keep and the capacity are at least 1")
@@ -577,16 +584,16 @@ def cache_evict(K, V, score, n_keep, lens=None, pos=None, n_first=0, n_recent=0,
                    "pos": torch.zeros(S, rows, dtype=torch.int32, device=K.device), "lens": torch.empty(S, dtype=torch.int32, device=K.device)}
         Ko, Vo, so, po, lo = out["k"], out["v"], out["score"], out.get("pos"), out.get("lens")
         rows = Ko.shape[1] if Ko.dim() == 3 else 0
-        _typed(what, K.dtype, V=V, k=Ko, v=Vo)
-        _typed(what, torch.float32, score=score, score_out=so)
-        _typed(what, torch.int32, pos=pos, lens=lens, pos_out=po, lens_out=lo)
-        _shaped(what, V=(V, (S, cap, d)), score=(score, (S, cap)), pos=(pos, (S, cap)), lens=(lens, (S,)), k=(Ko, (S, rows, d)), v=(Vo, (S, rows, d)),
-                score_out=(so, (S, rows)), pos_out=(po, (S, rows)), lens_out=(lo, (S,)))
-        _on_device(what, K.device, K=K, V=V, score=score, pos=pos, lens=lens, k=Ko, v=Vo, score_out=so, pos_out=po, lens_out=lo)
-        ws, size = _workspace(what, K.device, S, cap, n_keep, d, code, int(Ko.data_ptr() == K.data_ptr()))
-        _check(load().balancekv_cache_evict(K.data_ptr(), V.data_ptr(), score.data_ptr(), _ptr(pos), _ptr(lens), S, cap, Ko.data_ptr(), Vo.data_ptr(),
-                                            so.data_ptr(), _ptr(po), _ptr(lo), rows, n_keep, n_first, n_recent, d, code, _ptr(ws), size,
-                                            _stream_ptr(stream)), what)
+        _expect(what, device, "out k", Ko, dtype, (S, rows, d))
+        _expect(what, device, "out v", Vo, dtype, (S, rows, d))
+        _expect(what, device, "out score", so, torch.float32, (S, rows))
+        _expect(what, device, "out pos", po, torch.int32, (S, rows))
+        _expect(what, device, "out lens", lo, torch.int32, (S,))
+    size = _workspace_bytes(what, S, cap, n_keep, d, code, int(Ko.data_ptr() == K.data_ptr()))
+    ws = _workspace(K.device, size)
+    _check(load().balancekv_cache_evict(K.data_ptr(), V.data_ptr(), score.data_ptr(), _ptr(pos), _ptr(lens), S, cap, Ko.data_ptr(), Vo.data_ptr(),
+                                        so.data_ptr(), _ptr(po), _ptr(lo), rows, n_keep, n_first, n_recent, d, code, _ptr(ws), size,
+                                        _stream_ptr(None)), what)
     return out
 
 
@@ -598,25 +605,31 @@ def decode_attn_prefix(K_prefix, V_prefix, K, V, q, lens=None, weight=None, out=
     are in use); q: [n_seqs, n_kv_heads * group, d]."""
     import torch
 
+    if stream is not None:
+        with _on_stream(stream):
+            return decode_attn_prefix(K_prefix, V_prefix, K, V, q, lens, weight, out)
     what = "balancekv_decode_attn_prefix"
     if K_prefix.dim() != 3 or q.dim() != 3 or (K is None) != (V is None) or (K is not None and K.dim() != 4):
         raise ValueError(f"{what}: expected K_prefix [n_kv_heads, prefix_len, d], K [n_seqs, n_kv_heads, capacity, d] and q [n_seqs, n_q_heads, d]")
     (H, P, d), (B, Hq, _), cap = K_prefix.shape, q.shape, 0 if K is None else K.shape[2]
-    code = _dtype_code(what, K_prefix.dtype)
     if H < 1 or Hq % H:
         raise ValueError(f"{what}: {Hq} query heads do not share {H} KV heads")
-    _typed(what, K_prefix.dtype, V_prefix=V_prefix, K=K, V=V, q=q, out=out)
-    _typed(what, torch.float32, weight=weight)
-    _typed(what, torch.int32, lens=lens)
-    _shaped(what, V_prefix=(V_prefix, (H, P, d)), K=(K, (B, H, cap, d)), V=(V, (B, H, cap, d)), q=(q, (B, Hq, d)), weight=(weight, (H, P)),
-            lens=(lens, (B,)), out=(out, q.shape))
-    _on_device(what, K_prefix.device, K_prefix=K_prefix, V_prefix=V_prefix, K=K, V=V, q=q, lens=lens, weight=weight, out=out)
-    with _AllocateOn(stream):
-        if out is None:
-            out = torch.empty_like(q)
-        ws, size = _workspace(what, q.device, P, cap, B, H, Hq // H, d, code)
-        _check(load().balancekv_decode_attn_prefix(K_prefix.data_ptr(), V_prefix.data_ptr(), _ptr(weight), P, _ptr(K), _ptr(V), _ptr(lens), cap,
-                                                   q.data_ptr(), out.data_ptr(), B, H, Hq // H, d, code, _ptr(ws), size, _stream_ptr(stream)), what)
+    dtype, code, device = K_prefix.dtype, _dtype_code(what, K_prefix.dtype), K_prefix.get_device()
+    _expect(what, device, "K_prefix", K_prefix, dtype, (H, P, d))
+    _expect(what, device, "V_prefix", V_prefix, dtype, (H, P, d))
+    _expect(what, device, "K", K, dtype, (B, H, cap, d))
+    _expect(what, device, "V", V, dtype, (B, H, cap, d))
+    _expect(what, device, "q", q, dtype, (B, Hq, d))
+    _expect(what, device, "out", out, dtype, (B, Hq, d))
+    _expect(what, device, "weight", weight, torch.float32, (H, P))
+    _expect(what, device, "lens", lens, torch.int32, (B,))
+    _on_current(what, device, K_prefix)
+    if out is None:
+        out = torch.empty_like(q)
+    size = _workspace_bytes(what, P, cap, B, H, Hq // H, d, code)
+    ws = _workspace(q.device, size)
+    _check(load().balancekv_decode_attn_prefix(K_prefix.data_ptr(), V_prefix.data_ptr(), _ptr(weight), P, _ptr(K), _ptr(V), _ptr(lens), cap,
+                                               q.data_ptr(), out.data_ptr(), B, H, Hq // H, d, code, _ptr(ws), size, _stream_ptr(None)), what)
     return out
 
 

@@ -95,6 +95,8 @@ cudaError_t launch_score_simt(const AttnRows& A, const ScoreArgs& S, int d, int 
 int few_splits(int64_t streams, int cap);
 int64_t few_pitch(int cap);
 cudaError_t launch_attn_few(const AttnRows& A, float* x, int d, int is_bf16, cudaStream_t st);
+int few_cluster(int64_t streams, int cap, int n_rows, int d, int is_bf16);
+cudaError_t launch_attn_few_cluster(const AttnRows& A, const ScoreArgs& S, int C, int d, int is_bf16, cudaStream_t st);
 cudaError_t launch_few_end(const AttnRows& A, float* x, const ScoreArgs& S, int d, int is_bf16, cudaStream_t st);
 
 int attn_tc_splits(const AttnRows& A);

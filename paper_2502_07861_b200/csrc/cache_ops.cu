@@ -64,6 +64,7 @@ int plan_scored(AttnRows& A, float*& x, Pieces& ws, int n_streams, int capacity,
   A.total_rows = (int)rows * n_streams;
   A.scale = (float)(1.4426950408889634 / std::sqrt((double)head_dim));
   const bool few = rows <= kFewRows;
+  if (few && n_scored && few_cluster(n_streams, capacity, (int)rows, head_dim, dtype)) return BALANCEKV_OK;       // nothing leaves the chip
   A.n_slots = A.splits = few ? few_splits(n_streams, capacity) : dtype ? attn_tc_splits(A) : simt_splits((rows + 63) / 64 * n_streams, capacity);
   take_parts(A, ws, head_dim);
   if (n_scored) A.lse = ws.take<float>(A.total_rows);
@@ -152,7 +153,9 @@ extern "C" int balancekv_attn_scored(const void* K, const void* V, const int32_t
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   const ScoreArgs S{score_in, score_out, decay, n_scored};
   cudaError_t e;
-  if (A.n_rows <= kFewRows) {
+  if (const int C = A.n_rows <= kFewRows && n_scored ? few_cluster(n_streams, capacity, A.n_rows, head_dim, dtype) : 0) {
+    e = launch_attn_few_cluster(A, S, C, head_dim, dtype, st);
+  } else if (A.n_rows <= kFewRows) {
     e = launch_attn_few(A, x, head_dim, dtype, st);
     if (e == cudaSuccess && n_scored) e = launch_few_end(A, x, S, head_dim, dtype, st);
     else if (e == cudaSuccess && A.n_slots > 1) e = launch_attn_combine(A, head_dim, dtype, st);

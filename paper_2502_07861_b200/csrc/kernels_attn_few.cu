@@ -10,7 +10,10 @@
 // its warp has read the last.  bf16 tiles go through mma.sync with the cached rows as the M dimension and the queries as the eight
 // columns; fp32 tiles through FFMA, a lane per row for the logits and d / 32 columns per lane for the sums.
 // A bounded wait that gives up makes the results NaN.
+#include <cooperative_groups.h>
+
 #include <algorithm>
+#include <type_traits>
 
 #include "attn_rows.cuh"
 #include "tma_mma.cuh"
@@ -39,6 +42,11 @@ struct Few {
 struct FewArgs {
   AttnRows A;
   float* x;               // [n_streams, n_rows, pitch] logits; null: not wanted
+  int64_t pitch;
+};
+// Where the logits of a stream go: that of query row r and cached row i to x[r pitch + i]; null: nowhere.
+struct Logits {
+  float* x;
   int64_t pitch;
 };
 
@@ -91,8 +99,7 @@ __device__ inline uint32_t tile_off(int row, int piece) {
 
 // The warp's sums of its tiles, to mrg[row][kPitch].
 template <int D>
-__device__ inline void few_warp_bf16(const FewArgs& P, const Ring<true, D>& R, int s, int len, int n_tiles, int lane, int* abort_flag, float* mrg, bool& failed) {
-  const AttnRows& A = P.A;
+__device__ inline void few_warp_bf16(const AttnRows& A, const Logits& X, const Ring<true, D>& R, int s, int len, int n_tiles, int lane, int* abort_flag, float* mrg, bool& failed) {
   const int g = A.n_rows;
   // With up to four rows the columns 4-7 repeat the rows 0-3, and in the second product they carry the low parts of the weights:
   // one MMA then does what takes two with more rows.
@@ -114,7 +121,7 @@ __device__ inline void few_warp_bf16(const FewArgs& P, const Ring<true, D>& R, i
   for (int e = 0; e < 2; ++e) {
     const int h = packed ? (2 * tq + e) & 3 : 2 * tq + e;
     limit[e] = h < g ? attn_limit(A, len, h) : 0;
-    xs[e] = P.x && 2 * tq + e < g ? P.x + ((int64_t)s * g + h) * P.pitch : nullptr;
+    xs[e] = X.x && 2 * tq + e < g ? X.x + h * X.pitch : nullptr;
   }
   constexpr int kMB = D / 16;
   float o[kMB][4];                               // dim 16 mb + hq + 8 (j >> 1), query row 2 tq + (j & 1)
@@ -233,9 +240,8 @@ __device__ inline void few_warp_bf16(const FewArgs& P, const Ring<true, D>& R, i
 
 // The same with FFMA; kR >= n_rows rows.  qs: [kR][D], ps: [kR][32] of this warp.
 template <int D, int kR>
-__device__ inline void few_warp_fp32(const FewArgs& P, const Ring<false, D>& R, int s, int len, int n_tiles, int lane, int* abort_flag, const float* qs, float* ps,
+__device__ inline void few_warp_fp32(const AttnRows& A, const Logits& X, const Ring<false, D>& R, int s, int len, int n_tiles, int lane, int* abort_flag, const float* qs, float* ps,
                                      float* mrg, bool& failed) {
-  const AttnRows& A = P.A;
   const int g = A.n_rows;
   constexpr int kC = D / 32;                     // columns of a lane: kC lane ..
   float o[kR][kC], m[kR], l[kR];
@@ -271,7 +277,7 @@ __device__ inline void few_warp_fp32(const FewArgs& P, const Ring<false, D>& R, 
 #pragma unroll
     for (int r = 0; r < kR; ++r) {
       x[r] = row < limit[r] ? (acc[r].x + acc[r].y) * A.scale : -INFINITY;
-      if (P.x && r < g && row < len) P.x[((int64_t)s * g + r) * P.pitch + row] = x[r];
+      if (X.x && r < g && row < len) X.x[r * X.pitch + row] = x[r];
       more = more || x[r] > m[r];
     }
     if (__any_sync(0xffffffffu, more)) {
@@ -347,75 +353,185 @@ __device__ inline void few_warp_fp32(const FewArgs& P, const Ring<false, D>& R, 
   }
 }
 
+// What a CTA needs in shared memory besides the rings.
+template <bool kBf16, int D, int kR>
+struct FewShared {
+  uint64_t full[kWarps][Few<kBf16, D>::kRing];
+  int abort_flag;
+  __align__(16) float qs[kBf16 ? 4 : kR * D];
+  __align__(16) float ps[kBf16 ? 4 : kWarps * kR * 32];
+};
+
+// The CTA's share [t0, t1) of the tiles: every warp's sums, to mrg[warp][row][kPitch] in the rings' place.
+template <bool kBf16, int D, int kR>
+__device__ inline void few_tiles(const AttnRows& A, const Logits& X, const CUtensorMap& mk, const CUtensorMap& mv, FewShared<kBf16, D, kR>& sh, unsigned char* tiles,
+                                 int s, int len, int t0, int t1) {
+  using F = Few<kBf16, D>;
+  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+  const int n_tiles = max(0, (t1 - t0 - warp + kWarps - 1) / kWarps);
+  const Ring<kBf16, D> R{&mk, &mv, tiles + warp * F::kRing * F::kTileBytes, sh.full[warp], s, t0 + warp, 2 * n_tiles};
+  R.start(lane);
+  if constexpr (!kBf16) {
+    for (int i = tid; i < kR * D; i += kThreads)
+      sh.qs[i] = i / D < A.n_rows ? static_cast<const float*>(A.q)[attn_row(A, s, i / D) * D + i % D] : 0.f;
+    __syncthreads();
+  }
+  float* mrg = reinterpret_cast<float*>(tiles) + warp * kFewRows * F::kPitch;
+  bool failed = false;
+  if constexpr (kBf16) few_warp_bf16<D>(A, X, R, s, len, n_tiles, lane, &sh.abort_flag, mrg, failed);
+  else few_warp_fp32<D, kR>(A, X, R, s, len, n_tiles, lane, &sh.abort_flag, sh.qs, sh.ps + warp * kR * 32, mrg, failed);
+  if (failed && lane == 0) tc::st_release(&sh.abort_flag, 1);
+  __syncthreads();
+}
+
+template <bool kBf16, int D, int kR>
+__device__ inline void few_init(FewShared<kBf16, D, kR>& sh) {
+  if (threadIdx.x != 0) return;
+  for (int i = 0; i < kWarps * Few<kBf16, D>::kRing; ++i) tc::mbar_init(&sh.full[0][0] + i, 1);
+  sh.abort_flag = 0;
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+}
+
+// `n` sets of sums, the i-th at from(i)[kPitch], brought to one maximum and added by a warp: its lane's D / 32 columns.
+template <int D, int kMost, class From>
+__device__ inline void few_join(int n, int lane, From from, float (&acc)[D / 32], float& top, float& sum) {
+  constexpr int kC = D / 32;
+  float m[kMost], l[kMost], v[kMost][kC];
+  top = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < kMost; ++i) {
+    m[i] = -INFINITY;
+    l[i] = 0.f;
+    if (i < n) {
+      const float* at = from(i);
+      m[i] = at[D];
+      l[i] = at[D + 1];
+#pragma unroll
+      for (int c = 0; c < kC; ++c) v[i][c] = at[lane * kC + c];
+    }
+    top = fmaxf(top, m[i]);
+  }
+  const float base = top == -INFINITY ? 0.f : top;
+  sum = 0.f;
+#pragma unroll
+  for (int c = 0; c < kC; ++c) acc[c] = 0.f;
+#pragma unroll
+  for (int i = 0; i < kMost; ++i) {
+    if (i >= n) break;
+    const float f = exp2f(m[i] - base);
+    sum = fmaf(l[i], f, sum);
+#pragma unroll
+    for (int c = 0; c < kC; ++c) acc[c] = fmaf(v[i][c], f, acc[c]);
+  }
+}
+
+template <bool kBf16, int D>
+__device__ inline void few_put(const AttnRows& A, int64_t row, int lane, const float (&acc)[D / 32], float sum) {
+  constexpr int kC = D / 32;
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+  for (int c = 0; c < kC; c += 2) {
+    if constexpr (kBf16)
+      *reinterpret_cast<__nv_bfloat162*>(static_cast<__nv_bfloat16*>(A.out) + row * D + lane * kC + c) = __floats2bfloat162_rn(acc[c] * inv, acc[c + 1] * inv);
+    else
+      *reinterpret_cast<float2*>(static_cast<float*>(A.out) + row * D + lane * kC + c) = make_float2(acc[c] * inv, acc[c + 1] * inv);
+  }
+}
+
 // kR: rows that the fp32 form takes (bf16: 8).
 template <bool kBf16, int D, int kR>
 __global__ void __launch_bounds__(kThreads, (Few<kBf16, D>::kCtas)) attn_few_kernel(const __grid_constant__ FewArgs P, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv) {
   using F = Few<kBf16, D>;
   extern __shared__ unsigned char smem_raw[];
-  __shared__ uint64_t full[kWarps][F::kRing];
-  __shared__ int abort_flag;
-  __shared__ __align__(16) float qs[kBf16 ? 4 : kR * D];
-  __shared__ __align__(16) float ps[kBf16 ? 4 : kWarps * kR * 32];
+  __shared__ FewShared<kBf16, D, kR> sh;
   unsigned char* tiles = smem_raw + (-tc::smem_u32(smem_raw) & 1023u);
   const AttnRows& A = P.A;
-  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const int s = blockIdx.x, split = blockIdx.y;
-  if (tid == 0) {
-    for (int i = 0; i < kWarps * F::kRing; ++i) tc::mbar_init(&full[0][0] + i, 1);
-    abort_flag = 0;
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-  }
+  few_init(sh);
   grid_wait_and_release();
+  __syncthreads();
   const int len = attn_len(A, s), n_all = (len + kTile - 1) / kTile;
-  const int t0 = (int)((int64_t)n_all * split / A.splits), t1 = (int)((int64_t)n_all * (split + 1) / A.splits);
-  const int n_tiles = max(0, (t1 - t0 - warp + kWarps - 1) / kWarps);
-  if constexpr (!kBf16)
-    for (int i = tid; i < kR * D; i += kThreads)
-      qs[i] = i / D < A.n_rows ? static_cast<const float*>(A.q)[attn_row(A, s, i / D) * D + i % D] : 0.f;
-  __syncthreads();
-  const Ring<kBf16, D> R{&mk, &mv, tiles + warp * F::kRing * F::kTileBytes, full[warp], s, t0 + warp, 2 * n_tiles};
-  R.start(lane);
-  float* mrg = reinterpret_cast<float*>(tiles);  // [warp][row][kPitch], after the last tile
-  bool failed = false;
-  if constexpr (kBf16) few_warp_bf16<D>(P, R, s, len, n_tiles, lane, &abort_flag, mrg + warp * kFewRows * F::kPitch, failed);
-  else few_warp_fp32<D, kR>(P, R, s, len, n_tiles, lane, &abort_flag, qs, ps + warp * kR * 32, mrg + warp * kFewRows * F::kPitch, failed);
-  if (failed && lane == 0) tc::st_release(&abort_flag, 1);
-  __syncthreads();
-  // the warps' sums at one maximum
-  constexpr int kC = D / 32;
+  const Logits X{P.x ? P.x + (int64_t)s * A.n_rows * P.pitch : nullptr, P.pitch};
+  few_tiles(A, X, mk, mv, sh, tiles, s, len, (int)((int64_t)n_all * split / A.splits), (int)((int64_t)n_all * (split + 1) / A.splits));
+  const float* mrg = reinterpret_cast<const float*>(tiles);
   for (int r = warp; r < A.n_rows; r += kWarps) {
-    float top = -INFINITY, sum = 0.f, acc[kC] = {};
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) top = fmaxf(top, mrg[(w * kFewRows + r) * F::kPitch + D]);
-    const float base = top == -INFINITY ? 0.f : top;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-      const float* from = mrg + (w * kFewRows + r) * F::kPitch;
-      const float f = exp2f(from[D] - base);
-      sum = fmaf(from[D + 1], f, sum);
-#pragma unroll
-      for (int c = 0; c < kC; ++c) acc[c] = fmaf(from[lane * kC + c], f, acc[c]);
-    }
-    if (abort_flag) sum = NAN;
+    float acc[D / 32], top, sum;
+    few_join<D, kWarps>(kWarps, lane, [&](int w) { return mrg + (w * kFewRows + r) * F::kPitch; }, acc, top, sum);
+    if (sh.abort_flag) sum = NAN;
     const int64_t row = attn_row(A, s, r);
     if (A.n_slots > 1) {
       const int64_t at = (int64_t)(A.slot0 + split) * A.total_rows + row;
       if (lane == 0) A.part_ml[at] = make_float2(top, sum);
 #pragma unroll
-      for (int c = 0; c < kC; c += 2) *reinterpret_cast<float2*>(A.part + at * D + lane * kC + c) = make_float2(acc[c], acc[c + 1]);
+      for (int c = 0; c < D / 32; c += 2) *reinterpret_cast<float2*>(A.part + at * D + lane * (D / 32) + c) = make_float2(acc[c], acc[c + 1]);
       continue;
     }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    if (A.lse && lane == 0) A.lse[row] = sum == 0.f ? INFINITY : base + log2f(sum);
-#pragma unroll
-    for (int c = 0; c < kC; c += 2) {
-      if constexpr (kBf16)
-        *reinterpret_cast<__nv_bfloat162*>(static_cast<__nv_bfloat16*>(A.out) + row * D + lane * kC + c) = __floats2bfloat162_rn(acc[c] * inv, acc[c + 1] * inv);
-      else
-        *reinterpret_cast<float2*>(static_cast<float*>(A.out) + row * D + lane * kC + c) = make_float2(acc[c] * inv, acc[c + 1] * inv);
-    }
+    if (A.lse && lane == 0) A.lse[row] = sum == 0.f ? INFINITY : (top == -INFINITY ? 0.f : top) + log2f(sum);
+    few_put<kBf16, D>(A, row, lane, acc, sum);
   }
+}
+
+// The splits of a stream as a cluster of CTAs, where its logits fit their shared memory: they join their sums through it, every
+// CTA then turns its own logits into weights, and nothing but results leaves the chip.
+constexpr int kMaxCluster = 16;
+constexpr int logit_bytes(bool bf16, int d) { return !bf16 && d == 64 ? 8 * 1024 : 15 * 1024; }       // of a CTA: two (fp32, d = 128: one) still fit an SM
+
+template <bool kBf16, int D, int kR>
+__global__ void __launch_bounds__(kThreads, (Few<kBf16, D>::kCtas))
+attn_few_cluster_kernel(const __grid_constant__ AttnRows A, const ScoreArgs S, int pitch, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv) {
+  namespace cg = cooperative_groups;
+  using F = Few<kBf16, D>;
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ FewShared<kBf16, D, kR> sh;
+  __shared__ float lse[kFewRows];
+  unsigned char* tiles = smem_raw + (-tc::smem_u32(smem_raw) & 1023u);
+  float* x = reinterpret_cast<float*>(tiles + kWarps * F::kRing * F::kTileBytes);      // [n_rows][pitch]
+  float* joined = reinterpret_cast<float*>(tiles) + kWarps * kFewRows * F::kPitch;     // [n_rows][kPitch] of the CTA, behind its warps'
+  cg::cluster_group cluster = cg::this_cluster();
+  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+  const int C = (int)gridDim.y, c = blockIdx.y, s = blockIdx.x;
+  few_init(sh);
+  grid_wait_and_release();
+  __syncthreads();
+  const int len = attn_len(A, s), n_all = (len + kTile - 1) / kTile;
+  const int t0 = (int)((int64_t)n_all * c / C), t1 = (int)((int64_t)n_all * (c + 1) / C);
+  const int row0 = t0 * kTile, row1 = min(len, t1 * kTile);
+  few_tiles(A, Logits{x - row0, pitch}, mk, mv, sh, tiles, s, len, t0, t1);
+  const float* mrg = reinterpret_cast<const float*>(tiles);
+  for (int r = warp; r < A.n_rows; r += kWarps) {
+    float acc[D / 32], top, sum;
+    few_join<D, kWarps>(kWarps, lane, [&](int w) { return mrg + (w * kFewRows + r) * F::kPitch; }, acc, top, sum);
+    if (sh.abort_flag) sum = NAN;
+    float* to = joined + r * F::kPitch;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) to[lane * (D / 32) + i] = acc[i];
+    if (lane == 0) { to[D] = top; to[D + 1] = sum; }
+  }
+  cluster.sync();
+  // The rows' sums over the cluster: a lane per CTA.
+  for (int r = warp; r < A.n_rows; r += kWarps) {
+    const float* at = cluster.map_shared_rank(joined, lane < C ? lane : 0) + r * F::kPitch;
+    const float m = lane < C ? at[D] : -INFINITY, l = lane < C ? at[D + 1] : 0.f;
+    const float top = warp_max(m), base = top == -INFINITY ? 0.f : top, sum = warp_sum(l * exp2f(m - base));
+    const bool counted = r % A.n_queries >= A.n_queries - S.n_scored;
+    if (lane == 0) lse[r] = sum == 0.f || !counted ? INFINITY : base + log2f(sum);
+  }
+  // The outputs: row r by the warp r of the cluster's.
+  for (int r = c + C * warp; r < A.n_rows; r += C * kWarps) {
+    float acc[D / 32], top, sum;
+    few_join<D, kMaxCluster>(C, lane, [&](int b) { return cluster.map_shared_rank(joined, b) + r * F::kPitch; }, acc, top, sum);
+    few_put<kBf16, D>(A, attn_row(A, s, r), lane, acc, sum);
+  }
+  __syncthreads();
+  const int64_t first = (int64_t)s * A.cap;
+  for (int i = row0 + tid; i < row1; i += kThreads) {
+    float sum = 0.f;
+    for (int r = 0; r < A.n_rows; ++r) sum += exp2f(x[r * pitch + i - row0] - lse[r]);
+    score_put(S, first + i, sum);
+  }
+  cluster.sync();                                // nobody reads this CTA's sums any more
 }
 
 // Behind attn_few_kernel: the first `joins` CTAs join the splits, eight query rows each; the others turn 1024 logits per
@@ -435,18 +551,29 @@ __global__ void __launch_bounds__(kEndThreads) few_end_kernel(const __grid_const
   const int s = ((int)blockIdx.x - joins) / chunks, k0 = ((int)blockIdx.x - joins) % chunks * kEndKeys;
   const int len = attn_len(A, s);
   if (k0 >= len) return;
+  // what does not depend on the sums is asked for first
+  constexpr int kPer = kEndKeys / kEndThreads;
+  const float* x = P.x + (int64_t)s * A.n_rows * P.pitch + k0 + tid;
+  float logit[kFewRows][kPer];
+#pragma unroll
+  for (int r = 0; r < kFewRows; ++r)
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) logit[r][j] = r < A.n_rows && k0 + tid + j * kEndThreads < len ? x[r * P.pitch + j * kEndThreads] : -INFINITY;
   if (warp < A.n_rows) {                         // (eight warps, at most eight rows)
     const int64_t row = attn_row(A, s, warp);
     float v = 0.f;
     if (A.n_slots > 1) {
+      float2 ml[kAttnMaxSplits / 32];
       float top = -INFINITY, sum = 0.f;
-      for (int i = lane; i < A.n_slots; i += 32) top = fmaxf(top, A.part_ml[(int64_t)i * A.total_rows + row].x);
+#pragma unroll
+      for (int i = 0; i < kAttnMaxSplits / 32; ++i) {
+        ml[i] = lane + 32 * i < A.n_slots ? A.part_ml[(int64_t)(lane + 32 * i) * A.total_rows + row] : make_float2(-INFINITY, 0.f);
+        top = fmaxf(top, ml[i].x);
+      }
       top = warp_max(top);
       const float base = top == -INFINITY ? 0.f : top;
-      for (int i = lane; i < A.n_slots; i += 32) {
-        const float2 ml = A.part_ml[(int64_t)i * A.total_rows + row];
-        sum = fmaf(ml.y, exp2f(ml.x - base), sum);
-      }
+#pragma unroll
+      for (int i = 0; i < kAttnMaxSplits / 32; ++i) sum = fmaf(ml[i].y, exp2f(ml[i].x - base), sum);
       sum = warp_sum(sum);
       v = sum == 0.f ? INFINITY : base + log2f(sum);
     } else {
@@ -456,38 +583,69 @@ __global__ void __launch_bounds__(kEndThreads) few_end_kernel(const __grid_const
     if (lane == 0) lse[warp] = v;
   }
   __syncthreads();
-  const float* x = P.x + (int64_t)s * A.n_rows * P.pitch;
-  float sum[kEndKeys / kEndThreads] = {};
-  for (int r = 0; r < A.n_rows; ++r) {
+  float sum[kPer] = {};
+#pragma unroll
+  for (int r = 0; r < kFewRows; ++r) {
+    if (r >= A.n_rows) break;
     const float off = lse[r];
 #pragma unroll
-    for (int j = 0; j < kEndKeys / kEndThreads; ++j) {
-      const int key = k0 + tid + j * kEndThreads;
-      if (key < len) sum[j] += exp2f(x[r * P.pitch + key] - off);
-    }
+    for (int j = 0; j < kPer; ++j) sum[j] += exp2f(logit[r][j] - off);
   }
 #pragma unroll
-  for (int j = 0; j < kEndKeys / kEndThreads; ++j) {
+  for (int j = 0; j < kPer; ++j) {
     const int key = k0 + tid + j * kEndThreads;
     if (key < len) score_put(S, (int64_t)s * A.cap + key, sum[j]);
   }
 }
 
-template <bool kBf16, int D, int kR>
+// kR for the call's rows.
+template <bool kBf16, int D, class Run>
+cudaError_t for_rows(int n_rows, Run run) {
+  if constexpr (kBf16) return run(std::integral_constant<int, 8>{});
+  else return n_rows <= 2 ? run(std::integral_constant<int, 2>{}) : n_rows <= 4 ? run(std::integral_constant<int, 4>{}) : run(std::integral_constant<int, 8>{});
+}
+
+template <bool kBf16, int D>
 cudaError_t launch_few(const FewArgs& P, cudaStream_t st) {
   using F = Few<kBf16, D>;
   CUtensorMap mk, mv;
   const AttnRows& A = P.A;
   cudaError_t e = cache_map(&mk, A.K, kBf16, D, A.cap, A.n_streams, kTile);
   if (e == cudaSuccess) e = cache_map(&mv, A.V, kBf16, D, A.cap, A.n_streams, kTile);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_few_kernel<kBf16, D, kR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)F::kSmem);
   if (e != cudaSuccess) return e;
-  const PdlConfig pc(dim3(A.n_streams, A.splits), kThreads, F::kSmem, st);
-  return cudaLaunchKernelEx(&pc.cfg, attn_few_kernel<kBf16, D, kR>, P, mk, mv);
+  return for_rows<kBf16, D>(A.n_rows, [&](auto rows) {
+    auto kern = attn_few_kernel<kBf16, D, decltype(rows)::value>;
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)F::kSmem);
+    if (e != cudaSuccess) return e;
+    const PdlConfig pc(dim3(A.n_streams, A.splits), kThreads, F::kSmem, st);
+    return cudaLaunchKernelEx(&pc.cfg, kern, P, mk, mv);
+  });
 }
-template <int D>
-cudaError_t launch_few_fp32(const FewArgs& P, cudaStream_t st) {
-  return P.A.n_rows <= 2 ? launch_few<false, D, 2>(P, st) : P.A.n_rows <= 4 ? launch_few<false, D, 4>(P, st) : launch_few<false, D, 8>(P, st);
+
+int logit_pitch(int cap, int C) { return ((cap + kTile - 1) / kTile + C - 1) / C * kTile; }
+
+template <bool kBf16, int D>
+cudaError_t launch_cluster(const AttnRows& A, const ScoreArgs& S, int C, cudaStream_t st) {
+  using F = Few<kBf16, D>;
+  CUtensorMap mk, mv;
+  cudaError_t e = cache_map(&mk, A.K, kBf16, D, A.cap, A.n_streams, kTile);
+  if (e == cudaSuccess) e = cache_map(&mv, A.V, kBf16, D, A.cap, A.n_streams, kTile);
+  if (e != cudaSuccess) return e;
+  return for_rows<kBf16, D>(A.n_rows, [&](auto rows) {
+    auto kern = attn_few_cluster_kernel<kBf16, D, decltype(rows)::value>;
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)F::kSmem + logit_bytes(kBf16, D));
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess) return e;
+    const int pitch = logit_pitch(A.cap, C);
+    PdlConfig pc(dim3(A.n_streams, C), kThreads, F::kSmem + (size_t)A.n_rows * pitch * 4, st);
+    cudaLaunchAttribute attrs[2] = {pc.attr, {}};
+    attrs[1].id = cudaLaunchAttributeClusterDimension;
+    attrs[1].val.clusterDim.x = attrs[1].val.clusterDim.z = 1;
+    attrs[1].val.clusterDim.y = C;
+    pc.cfg.attrs = attrs;
+    pc.cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&pc.cfg, kern, A, S, pitch, mk, mv);
+  });
 }
 template <bool kBf16, int D>
 cudaError_t launch_end(const FewArgs& P, const ScoreArgs& S, cudaStream_t st) {
@@ -506,13 +664,27 @@ int few_splits(int64_t streams, int cap) {
   return (int)std::max<int64_t>(1, std::min<int64_t>({want, most, (int64_t)kAttnMaxSplits}));
 }
 
+// CTAs of a stream's cluster, 0 where its logits do not fit or the clusters do not fit one wave: as many as leave a tile for every warp.
+// (256 streams of up to 8192 rows in clusters of 16 took 228 us, as splits of a launch 108: clusters start and end as a whole.)
+int few_cluster(int64_t streams, int cap, int n_rows, int d, int is_bf16) {
+  int C = 1;
+  while (C < kMaxCluster && 2 * streams * C <= 2 * kAttnSms && cap > C * kWarps * kTile) C *= 2;
+  return streams * C <= 2 * kAttnSms && (int64_t)n_rows * logit_pitch(cap, C) * 4 <= logit_bytes(is_bf16, d) ? C : 0;
+}
+
 int64_t few_pitch(int cap) { return ((int64_t)cap + 31) / 32 * 32; }
 
 // x: [n_streams, n_rows, few_pitch(cap)] where launch_few_end is to follow, else null.
 cudaError_t launch_attn_few(const AttnRows& A, float* x, int d, int is_bf16, cudaStream_t st) {
   const FewArgs P{A, x, few_pitch(A.cap)};
-  if (is_bf16) return d == 128 ? launch_few<true, 128, 8>(P, st) : launch_few<true, 64, 8>(P, st);
-  return d == 128 ? launch_few_fp32<128>(P, st) : launch_few_fp32<64>(P, st);
+  if (is_bf16) return d == 128 ? launch_few<true, 128>(P, st) : launch_few<true, 64>(P, st);
+  return d == 128 ? launch_few<false, 128>(P, st) : launch_few<false, 64>(P, st);
+}
+
+// Outputs and scores by clusters of C CTAs.
+cudaError_t launch_attn_few_cluster(const AttnRows& A, const ScoreArgs& S, int C, int d, int is_bf16, cudaStream_t st) {
+  if (is_bf16) return d == 128 ? launch_cluster<true, 128>(A, S, C, st) : launch_cluster<true, 64>(A, S, C, st);
+  return d == 128 ? launch_cluster<false, 128>(A, S, C, st) : launch_cluster<false, 64>(A, S, C, st);
 }
 
 // The scores, and the outputs where there are several splits.

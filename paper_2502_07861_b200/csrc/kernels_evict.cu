@@ -31,7 +31,7 @@ __device__ inline uint32_t score_key(float x) {
 
 __global__ void __launch_bounds__(kThreads) evict_select_kernel(const EvictArgs E, int per, int staged) {
   extern __shared__ uint32_t keys[];
-  __shared__ uint32_t hist[kPasses][kBins];
+  __shared__ __align__(16) uint32_t hist[kPasses][kBins];
   __shared__ int warp_n[kWarps], warp_m[kWarps], scan[kWarps];
   __shared__ int cta_newest, cta_eq, cta_holes, cta_movers, found, above;
   cg::cluster_group cluster = cg::this_cluster();
@@ -97,12 +97,17 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const EvictArgs 
     constexpr int kPer = kBins / kThreads;
     int n[kPer], sum = 0;
     const int top = kBins - 1 - kPer * tid;
+    static_assert(kPer == 4, "a 16-byte load of the other CTAs' bins");
 #pragma unroll
     for (int j = 0; j < kPer; ++j) n[j] = 0;
-    for (int b = 0; b < C; ++b) {
-      const uint32_t* h = cluster.map_shared_rank(&hist[pass][0], b);
 #pragma unroll
-      for (int j = 0; j < kPer; ++j) n[j] += (int)h[top - j];
+    for (int b = 0; b < kMaxCluster; ++b) {
+      if (b >= C) break;
+      const uint4 h = *reinterpret_cast<const uint4*>(cluster.map_shared_rank(&hist[pass][0], b) + top - 3);
+      n[0] += (int)h.w;
+      n[1] += (int)h.z;
+      n[2] += (int)h.y;
+      n[3] += (int)h.x;
     }
 #pragma unroll
     for (int j = 0; j < kPer; ++j) sum += n[j];

@@ -179,7 +179,7 @@ score_tc_kernel(const __grid_constant__ AttnRows A, const ScoreArgs C, int block
                 part.y += (q + 1 >= from ? ex2(lo.y) : 0.f) + (q + 3 >= from ? ex2(hi.y) : 0.f);
               } else {
                 part = __fadd2_rn(part, make_float2(ex2(lo.x), ex2(lo.y)));
-                part = __fadd2_rn(part, (k / 4) % 4 == 3 ? make_float2(ex2(hi.x), ex2(hi.y)) : exp2_fma(hi));
+                part = __fadd2_rn(part, (k / 4) % 4 == 3 ? make_float2(ex2(hi.x), ex2(hi.y)) : exp2_fma(hi));    // three of eight pairs
               }
             }
         };

@@ -53,7 +53,7 @@ def test_small_workspaces_are_refused(name):
 
 
 def test_workspaces_follow_from_the_arguments():
-    rc, one = _workspace("balancekv_attn_scored", 8, 4096, 1, 4, 128, 1, 1)
+    rc, one = _workspace("balancekv_attn_scored", 8, 1 << 20, 1, 4, 128, 1, 1)
     assert rc == OK and one > 0
     rc, none = _workspace("balancekv_attn_scored", 1024, 64, 1, 4, 128, 1, 0)
     assert rc == OK and none == 0                          # one split, no scores: nothing to keep between kernels
