@@ -10,7 +10,7 @@ namespace bkv {
 
 constexpr int kAttnSms = 148;                 // split factors and workspaces follow from sizes alone
 constexpr int kAttnMaxSplits = 64;
-constexpr int kFewRows = 8;                   // query rows of a stream that the one-pass decode kernels take
+constexpr int kFewRows = 8;                   // query rows that a CTA of the one-pass decode kernels takes
 
 struct AttnRows {
   const void *K, *V;        // [n_streams, cap, d]
@@ -55,28 +55,76 @@ __device__ inline void score_put(const ScoreArgs& S, int64_t at, float sum) {
   S.out[at] = S.in ? fmaf(S.decay, S.in[at], sum) : sum;
 }
 
-// A warp per query row: the slots' sums brought to one maximum and added, in the order of the slots.
+// Joining the slots of query rows: their sums brought to one maximum and added.  A CTA of eight warps takes eight rows, or, of more than
+// eight slots, two rows with four warps each, which add every fourth slot up and then one another's sums: the order depends on sizes alone.
+constexpr int kJoinThreads = 256, kJoinMaxSlots = 2 * kAttnMaxSplits;
+__host__ __device__ inline int join_rows(const AttnRows& A) { return A.n_slots > 8 ? 2 : 8; }
+inline int join_ctas(const AttnRows& A) { return (A.total_rows + join_rows(A) - 1) / join_rows(A); }
+template <int D>
+struct JoinShared {
+  float acc[kJoinThreads / 32][D];
+};
 template <bool kBf16, int D>
-__device__ inline void join_splits(const AttnRows& A, int64_t row, int lane) {
-  float top = -INFINITY;
-  for (int i = lane; i < A.n_slots; i += 32) top = fmaxf(top, A.part_ml[(int64_t)i * A.total_rows + row].x);
-  top = warp_max(top);
-  const float base = top == -INFINITY ? 0.f : top;
-  constexpr int kPer = D / 32;
-  float sum = 0.f, acc[kPer] = {};
-#pragma unroll 4
-  for (int i = 0; i < A.n_slots; ++i) {
-    const int64_t at = (int64_t)i * A.total_rows + row;
-    const float2 ml = A.part_ml[at];
-    const float f = exp2f(ml.x - base);
-    sum = fmaf(ml.y, f, sum);
+__device__ inline void join_splits(const AttnRows& A, int cta, JoinShared<D>& sh) {
+  constexpr int kPer = D / 32, kChunks = kJoinMaxSlots / 32, kAhead = 8;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, rows = join_rows(A), ways = kJoinThreads / 32 / rows, way = warp % ways;
+  const int64_t row = (int64_t)cta * rows + warp / ways;
+  const bool held = row < A.total_rows;
+  float acc[kPer] = {}, sum = 0.f, base = 0.f;
+  if (held) {
+    float2 ml[kChunks];
+    float top = -INFINITY, f[kChunks];
 #pragma unroll
-    for (int c = 0; c < kPer; c += 2) {
-      const float2 v = *reinterpret_cast<const float2*>(A.part + at * D + kPer * lane + c);
-      acc[c] = fmaf(v.x, f, acc[c]);
-      acc[c + 1] = fmaf(v.y, f, acc[c + 1]);
+    for (int k = 0; k < kChunks; ++k) {
+      ml[k] = lane + 32 * k < A.n_slots ? A.part_ml[(int64_t)(lane + 32 * k) * A.total_rows + row] : make_float2(-INFINITY, 0.f);
+      top = fmaxf(top, ml[k].x);
+    }
+    top = warp_max(top);
+    base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+    for (int k = 0; k < kChunks; ++k) {
+      f[k] = exp2f(ml[k].x - base);
+      sum = fmaf(ml[k].y, f[k], sum);
+    }
+    sum = warp_sum(sum);
+#pragma unroll
+    for (int k = 0; k < kChunks; ++k) {
+      for (int i0 = 32 * k + way; i0 < min(32 * k + 32, A.n_slots); i0 += kAhead * ways) {
+        float v[kAhead][kPer];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+          const int i = i0 + j * ways;
+          const float* from = A.part + ((int64_t)i * A.total_rows + row) * D + kPer * lane;
+          const bool in = i < min(32 * k + 32, A.n_slots);
+#pragma unroll
+          for (int c = 0; c < kPer; c += 2) {
+            const float2 x = in ? *reinterpret_cast<const float2*>(from + c) : make_float2(0.f, 0.f);
+            v[j][c] = x.x;
+            v[j][c + 1] = x.y;
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+          const float w = __shfl_sync(0xffffffffu, f[k], i0 + j * ways & 31);
+          if (i0 + j * ways >= min(32 * k + 32, A.n_slots)) break;
+#pragma unroll
+          for (int c = 0; c < kPer; ++c) acc[c] = fmaf(v[j][c], w, acc[c]);
+        }
+      }
     }
   }
+  if (ways > 1) {
+#pragma unroll
+    for (int c = 0; c < kPer; ++c) sh.acc[warp][kPer * lane + c] = acc[c];
+    __syncthreads();
+    if (way != 0) return;
+#pragma unroll
+    for (int c = 0; c < kPer; ++c) {
+      acc[c] = 0.f;
+      for (int w = 0; w < ways; ++w) acc[c] += sh.acc[warp + w][kPer * lane + c];
+    }
+  }
+  if (!held) return;
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   if (A.lse && lane == 0) A.lse[row] = sum == 0.f ? INFINITY : base + log2f(sum);
 #pragma unroll
@@ -92,14 +140,16 @@ cudaError_t launch_attn_simt(const AttnRows& A, int d, int is_bf16, cudaStream_t
 cudaError_t launch_attn_combine(const AttnRows& A, int d, int is_bf16, cudaStream_t st);
 cudaError_t launch_score_simt(const AttnRows& A, const ScoreArgs& S, int d, int is_bf16, cudaStream_t st);
 
-int few_splits(int64_t streams, int cap);
+int few_splits(int64_t streams, int cap, int n_rows);
 int64_t few_pitch(int cap);
-cudaError_t launch_attn_few(const AttnRows& A, float* x, int d, int is_bf16, cudaStream_t st);
+cudaError_t launch_attn_few(const AttnRows& A, float* x, const AttnRows* also, int d, int is_bf16, cudaStream_t st);
 int few_cluster(int64_t streams, int cap, int n_rows, int d, int is_bf16);
-cudaError_t launch_attn_few_cluster(const AttnRows& A, const ScoreArgs& S, int C, int d, int is_bf16, cudaStream_t st);
+int64_t few_cluster_sums(const AttnRows& A);
+cudaError_t launch_attn_few_cluster(const AttnRows& A, const ScoreArgs& S, int C, float* sums, int d, int is_bf16, cudaStream_t st);
 cudaError_t launch_few_end(const AttnRows& A, float* x, const ScoreArgs& S, int d, int is_bf16, cudaStream_t st);
 
 int attn_tc_splits(const AttnRows& A);
+int attn_tc_slots(const AttnRows& A, int splits);
 cudaError_t launch_attn_tc(const AttnRows& A, int d, cudaStream_t st);
 cudaError_t launch_score_tc(const AttnRows& A, const ScoreArgs& S, int d, cudaStream_t st);
 

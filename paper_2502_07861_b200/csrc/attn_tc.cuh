@@ -37,6 +37,21 @@ __device__ inline void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
 }
 __device__ inline void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+__device__ inline float max3(float a, float b, float c) {
+  float y;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
+}
+template <int N>
+__device__ inline float max_of(const float (&x)[N]) {
+  float a = x[0], b = x[1];
+#pragma unroll
+  for (int i = 2; i < N; i += 4) {
+    a = max3(a, x[i], x[i + 1]);
+    if (i + 3 < N) b = max3(b, x[i + 2], x[i + 3]);
+  }
+  return fmaxf(a, b);
+}
 __device__ inline float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

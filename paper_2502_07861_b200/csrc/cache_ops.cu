@@ -49,7 +49,12 @@ void take_parts(AttnRows& A, Pieces& ws, int d) {
 
 // ---- attn_scored
 
-// x: the logits that the one-pass kernels leave for the scores.
+// CTAs of a cluster where clusters serve the call, else 0.
+int cluster_of(const AttnRows& A, int n_scored, int head_dim, int dtype) {
+  return n_scored ? few_cluster(A.n_streams, A.cap, A.n_rows, head_dim, dtype) : 0;
+}
+
+// x: what the one-pass kernels leave for the scores.
 int plan_scored(AttnRows& A, float*& x, Pieces& ws, int n_streams, int capacity, int n_queries, int group, int head_dim, int dtype, int n_scored) {
   if (n_streams < 1 || capacity < 1 || n_queries < 1 || group < 1 || group > kMaxGroup || !shape_ok(head_dim, dtype)) return BALANCEKV_E_INVAL;
   if (n_scored < 0 || n_scored > n_queries) return BALANCEKV_E_INVAL;
@@ -64,8 +69,12 @@ int plan_scored(AttnRows& A, float*& x, Pieces& ws, int n_streams, int capacity,
   A.total_rows = (int)rows * n_streams;
   A.scale = (float)(1.4426950408889634 / std::sqrt((double)head_dim));
   const bool few = rows <= kFewRows;
-  if (few && n_scored && few_cluster(n_streams, capacity, (int)rows, head_dim, dtype)) return BALANCEKV_OK;       // nothing leaves the chip
-  A.n_slots = A.splits = few ? few_splits(n_streams, capacity) : dtype ? attn_tc_splits(A) : simt_splits((rows + 63) / 64 * n_streams, capacity);
+  if (cluster_of(A, n_scored, head_dim, dtype)) {        // nothing leaves the chip but what groups of query rows add up
+    x = ws.take<float>(few_cluster_sums(A));
+    return BALANCEKV_OK;
+  }
+  A.splits = few ? few_splits(n_streams, capacity, (int)rows) : dtype ? attn_tc_splits(A) : simt_splits((rows + 63) / 64 * n_streams, capacity);
+  A.n_slots = !few && dtype ? attn_tc_slots(A, A.splits) : A.splits;
   take_parts(A, ws, head_dim);
   if (n_scored) A.lse = ws.take<float>(A.total_rows);
   x = n_scored && few ? ws.take<float>(A.total_rows * few_pitch(capacity)) : nullptr;
@@ -73,6 +82,10 @@ int plan_scored(AttnRows& A, float*& x, Pieces& ws, int n_streams, int capacity,
 }
 
 // ---- decode_attn_prefix
+
+// Whether the one-pass kernels take the prefix, eight query rows to a CTA: fp32 has no tensor cores to go to, and its tiles of 64 query
+// rows pay only when there are a few of them.
+bool prefix_by_few(const AttnRows& P, int dtype) { return P.n_rows <= (dtype ? kFewRows : 128); }
 
 int plan_prefix(AttnRows& P, AttnRows& A, Pieces& ws, int prefix_len, int capacity, int n_seqs, int n_kv_heads, int group, int head_dim, int dtype) {
   if (prefix_len < 1 || capacity < 0 || n_seqs < 1 || n_kv_heads < 1 || group < 1 || group > kMaxGroup || !shape_ok(head_dim, dtype)) return BALANCEKV_E_INVAL;
@@ -88,14 +101,15 @@ int plan_prefix(AttnRows& P, AttnRows& A, Pieces& ws, int prefix_len, int capaci
   P.n_rows = n_seqs * group;
   P.q_stream = P.q_inner = group;
   P.q_outer = n_kv_heads * group;
-  P.splits = dtype ? attn_tc_splits(P) : simt_splits((int64_t)(P.n_rows + 63) / 64 * n_kv_heads, prefix_len);
+  const bool few = prefix_by_few(P, dtype);
+  P.splits = few ? few_splits(n_kv_heads, prefix_len, P.n_rows) : dtype ? attn_tc_splits(P) : simt_splits((int64_t)(P.n_rows + 63) / 64 * n_kv_heads, prefix_len);
   A.n_streams = (int)streams;                  // a sequence's own rows
   A.lens_div = n_kv_heads;
   A.cap = capacity;
   A.n_rows = A.q_stream = A.q_inner = group;
-  A.splits = capacity ? few_splits(streams, capacity) : 0;
-  A.slot0 = P.splits;
-  P.n_slots = A.n_slots = P.splits + A.splits;
+  A.splits = capacity ? few_splits(streams, capacity, group) : 0;
+  A.slot0 = !few && dtype ? attn_tc_slots(P, P.splits) : P.splits;
+  P.n_slots = A.n_slots = A.slot0 + A.splits;
   take_parts(P, ws, head_dim);
   A.part = P.part;
   A.part_ml = P.part_ml;
@@ -153,10 +167,10 @@ extern "C" int balancekv_attn_scored(const void* K, const void* V, const int32_t
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   const ScoreArgs S{score_in, score_out, decay, n_scored};
   cudaError_t e;
-  if (const int C = A.n_rows <= kFewRows && n_scored ? few_cluster(n_streams, capacity, A.n_rows, head_dim, dtype) : 0) {
-    e = launch_attn_few_cluster(A, S, C, head_dim, dtype, st);
+  if (const int C = cluster_of(A, n_scored, head_dim, dtype)) {
+    e = launch_attn_few_cluster(A, S, C, x, head_dim, dtype, st);
   } else if (A.n_rows <= kFewRows) {
-    e = launch_attn_few(A, x, head_dim, dtype, st);
+    e = launch_attn_few(A, x, nullptr, head_dim, dtype, st);
     if (e == cudaSuccess && n_scored) e = launch_few_end(A, x, S, head_dim, dtype, st);
     else if (e == cudaSuccess && A.n_slots > 1) e = launch_attn_combine(A, head_dim, dtype, st);
   } else {
@@ -198,8 +212,13 @@ extern "C" int balancekv_decode_attn_prefix(const void* K_prefix, const void* V_
   P.q = A.q = q;
   P.out = A.out = out;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  cudaError_t e = dtype ? launch_attn_tc(P, head_dim, st) : launch_attn_simt(P, head_dim, dtype, st);
-  if (e == cudaSuccess && A.splits) e = launch_attn_few(A, nullptr, head_dim, dtype, st);
+  cudaError_t e;
+  if (prefix_by_few(P, dtype)) {
+    e = launch_attn_few(P, nullptr, A.splits ? &A : nullptr, head_dim, dtype, st);
+  } else {
+    e = dtype ? launch_attn_tc(P, head_dim, st) : launch_attn_simt(P, head_dim, dtype, st);
+    if (e == cudaSuccess && A.splits) e = launch_attn_few(A, nullptr, nullptr, head_dim, dtype, st);
+  }
   if (e == cudaSuccess && P.n_slots > 1) e = launch_attn_combine(P, head_dim, dtype, st);
   return report("balancekv_decode_attn_prefix", e);
 }

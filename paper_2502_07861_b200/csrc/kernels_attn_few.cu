@@ -1,11 +1,11 @@
-// Attention of up to eight query rows per stream over a caller-held cache: one pass at memory speed, split over the rows.
+// Attention of few query rows per stream over a caller-held cache: one pass at memory speed, split over the cached rows.
 //
-//   x_{r,i} = <q_r, k_i> log2(e) / sqrt d,   out_r = sum_i 2^(x_{r,i} - m_r) v_i / sum_i 2^(x_{r,i} - m_r)
+//   x_{r,i} = <q_r, k_i> log2(e) / sqrt d + log2 w_i,   out_r = sum_i 2^(x_{r,i} - m_r) v_i / sum_i 2^(x_{r,i} - m_r)
 //
 // and where the rows are scored, the weights of every cached row: they need the finished sums of all splits, so the logits leave as
 // fp32 (4 bytes per row and query against 2 d elements read) and a second launch turns them into weights while it joins the splits.
 //
-// A CTA is four warps, each with a ring of its own of tiles of 32 rows that TMA fills (K and V tiles in turn, boxes of 128 bytes x
+// A CTA takes up to eight query rows and is four warps, each with a ring of its own of tiles of 32 rows that TMA fills (K and V tiles in turn, boxes of 128 bytes x
 // 32 rows, 128-byte swizzle): a warp waits for nothing but its own copies, and the lane that asks for the next tile does so as soon as
 // its warp has read the last.  bf16 tiles go through mma.sync with the cached rows as the M dimension and the queries as the eight
 // columns; fp32 tiles through FFMA, a lane per row for the logits and d / 32 columns per lane for the sums.
@@ -13,6 +13,7 @@
 #include <cooperative_groups.h>
 
 #include <algorithm>
+#include <climits>
 #include <type_traits>
 
 #include "attn_rows.cuh"
@@ -44,7 +45,20 @@ struct FewArgs {
   float* x;               // [n_streams, n_rows, pitch] logits; null: not wanted
   int64_t pitch;
 };
-// Where the logits of a stream go: that of query row r and cached row i to x[r pitch + i]; null: nowhere.
+// What a launch does: one set of streams, or two (a shared prefix and the sequences' own rows).
+struct FewJobs {
+  FewArgs job[2];
+  int32_t groups[2];      // of eight query rows
+  int32_t ctas0;          // CTAs of the first set
+};
+struct FewMaps {
+  CUtensorMap k[2], v[2];
+};
+// The query rows r0 .. r0 + g - 1 of a stream.
+struct Group {
+  int32_t r0, g;
+};
+// Where their logits go: that of row r0 + r and cached row i to x[r pitch + i]; null: nowhere.
 struct Logits {
   float* x;
   int64_t pitch;
@@ -97,10 +111,26 @@ __device__ inline uint32_t tile_off(int row, int piece) {
   return (uint32_t)(piece >> 3) * kBox + (uint32_t)row * 128u + (uint32_t)(((piece & 7) ^ (row & 7)) << 4);
 }
 
+// Of a warp's tile: the lane's row's log weight, and which rows count (none behind the last, none of weight zero), by bit.  The weight
+// of the next tile is asked for a tile ahead.
+struct TileWeights {
+  const float* w;                                // of the stream; null: ones
+  float next = 1.f;
+  __device__ void ask(int row, int len) {
+    if (w) next = row < len ? w[row] : 0.f;
+  }
+  __device__ uint32_t take(int rows, float& log_w) const {
+    log_w = w ? log2f(next) : 0.f;
+    const uint32_t held = rows >= kTile ? 0xffffffffu : (1u << rows) - 1u;
+    return w ? held & __ballot_sync(0xffffffffu, !(next == 0.f)) : held;
+  }
+};
+
 // The warp's sums of its tiles, to mrg[row][kPitch].
 template <int D>
-__device__ inline void few_warp_bf16(const AttnRows& A, const Logits& X, const Ring<true, D>& R, int s, int len, int n_tiles, int lane, int* abort_flag, float* mrg, bool& failed) {
-  const int g = A.n_rows;
+__device__ inline void few_warp_bf16(const AttnRows& A, const Group& G, const Logits& X, const Ring<true, D>& R, int s, int len, int n_tiles, int lane, int* abort_flag,
+                                     float* mrg, bool& failed) {
+  const int g = G.g;
   // With up to four rows the columns 4-7 repeat the rows 0-3, and in the second product they carry the low parts of the weights:
   // one MMA then does what takes two with more rows.
   const bool packed = g <= 4;
@@ -108,7 +138,7 @@ __device__ inline void few_warp_bf16(const AttnRows& A, const Logits& X, const R
   uint32_t qb[D / 16][2];
   {
     const int hr = packed ? hq & 3 : hq;
-    const __nv_bfloat16* qp = static_cast<const __nv_bfloat16*>(A.q) + (hr < g ? attn_row(A, s, hr) : 0) * D;
+    const __nv_bfloat16* qp = static_cast<const __nv_bfloat16*>(A.q) + (hr < g ? attn_row(A, s, G.r0 + hr) : 0) * D;
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) {
       qb[ks][0] = hr < g ? *reinterpret_cast<const uint32_t*>(qp + ks * 16 + 2 * tq) : 0u;
@@ -120,7 +150,7 @@ __device__ inline void few_warp_bf16(const AttnRows& A, const Logits& X, const R
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
     const int h = packed ? (2 * tq + e) & 3 : 2 * tq + e;
-    limit[e] = h < g ? attn_limit(A, len, h) : 0;
+    limit[e] = h < g ? attn_limit(A, len, G.r0 + h) : 0;
     xs[e] = X.x && 2 * tq + e < g ? X.x + h * X.pitch : nullptr;
   }
   constexpr int kMB = D / 16;
@@ -131,8 +161,13 @@ __device__ inline void few_warp_bf16(const AttnRows& A, const Logits& X, const R
   const int mi = lane >> 3, mr = lane & 7;
   const int k_row = (mi & 1) * 8 + mr, k_piece = mi >> 1;
   const int v_row = (mi >> 1) * 8 + mr, v_piece = mi & 1;
+  TileWeights W{A.w ? A.w + (int64_t)s * A.cap : nullptr};
+  W.ask(R.first_tile * kTile + lane, len);
   for (int n = 0; n < n_tiles; ++n) {
     const int row0 = (R.first_tile + n * kWarps) * kTile, rows = min(kTile, len - row0);
+    float log_w;
+    const uint32_t alive = W.take(rows, log_w);
+    W.ask(row0 + kWarps * kTile + lane, len);
     if (!R.wait(2 * n, lane, abort_flag)) { R.drain(2 * n, lane); failed = true; break; }
     const uint32_t Kt = tc::smem_u32(R.at(2 * n));
     float sa[2][4][4];
@@ -158,8 +193,9 @@ __device__ inline void few_warp_bf16(const AttnRows& A, const Logits& X, const R
     for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int row = row0 + 16 * tb + hq + 8 * (j >> 1);
-        x[tb][j] = row < limit[j & 1] ? ((sa[tb][0][j] + sa[tb][1][j]) + (sa[tb][2][j] + sa[tb][3][j])) * A.scale : -INFINITY;
+        const int in_tile = 16 * tb + hq + 8 * (j >> 1), row = row0 + in_tile;
+        const float lw = A.w ? __shfl_sync(0xffffffffu, log_w, in_tile) : 0.f;
+        x[tb][j] = row < limit[j & 1] && (alive >> in_tile & 1u) ? fmaf((sa[tb][0][j] + sa[tb][1][j]) + (sa[tb][2][j] + sa[tb][3][j]), A.scale, lw) : -INFINITY;
         if (xs[j & 1] && row < len) xs[j & 1][row] = x[tb][j];
         mx[j & 1] = fmaxf(mx[j & 1], x[tb][j]);
       }
@@ -202,7 +238,9 @@ __device__ inline void few_warp_bf16(const AttnRows& A, const Logits& X, const R
     const uint32_t Vt = tc::smem_u32(R.at(2 * n + 1));
 #pragma unroll
     for (int tb = 0; tb < 2; ++tb) {
-      const int row = min(v_row + 16 * tb, rows - 1);      // behind the last row that row again, times zero: what is there may be anything
+      // a row that does not count is replaced by one that does, times zero: what it holds may be anything
+      const int row = alive >> (v_row + 16 * tb) & 1u ? v_row + 16 * tb : __ffs(alive) - 1;
+      if (alive == 0) break;
       uint32_t va[kMB][4];
 #pragma unroll
       for (int mb = 0; mb < kMB; ++mb) ldsm_x4_trans(Vt + tile_off(row, mb * 2 + v_piece), va[mb]);
@@ -238,11 +276,11 @@ __device__ inline void few_warp_bf16(const AttnRows& A, const Logits& X, const R
   }
 }
 
-// The same with FFMA; kR >= n_rows rows.  qs: [kR][D], ps: [kR][32] of this warp.
+// The same with FFMA; kR >= g rows.  qs: [kR][D], ps: [kR][32] of this warp.
 template <int D, int kR>
-__device__ inline void few_warp_fp32(const AttnRows& A, const Logits& X, const Ring<false, D>& R, int s, int len, int n_tiles, int lane, int* abort_flag, const float* qs, float* ps,
+__device__ inline void few_warp_fp32(const AttnRows& A, const Group& G, const Logits& X, const Ring<false, D>& R, int s, int len, int n_tiles, int lane, int* abort_flag, const float* qs, float* ps,
                                      float* mrg, bool& failed) {
-  const int g = A.n_rows;
+  const int g = G.g;
   constexpr int kC = D / 32;                     // columns of a lane: kC lane ..
   float o[kR][kC], m[kR], l[kR];
   int limit[kR];
@@ -250,12 +288,17 @@ __device__ inline void few_warp_fp32(const AttnRows& A, const Logits& X, const R
   for (int r = 0; r < kR; ++r) {
     m[r] = -INFINITY;
     l[r] = 0.f;
-    limit[r] = r < g ? attn_limit(A, len, r) : 0;
+    limit[r] = r < g ? attn_limit(A, len, G.r0 + r) : 0;
 #pragma unroll
     for (int c = 0; c < kC; ++c) o[r][c] = 0.f;
   }
+  TileWeights W{A.w ? A.w + (int64_t)s * A.cap : nullptr};
+  W.ask(R.first_tile * kTile + lane, len);
   for (int n = 0; n < n_tiles; ++n) {
-    const int row0 = (R.first_tile + n * kWarps) * kTile, rows = min(kTile, len - row0), row = row0 + lane;
+    const int row0 = (R.first_tile + n * kWarps) * kTile, row = row0 + lane;
+    float log_w;
+    const uint32_t alive = W.take(len - row0, log_w);
+    W.ask(row + kWarps * kTile, len);
     if (!R.wait(2 * n, lane, abort_flag)) { R.drain(2 * n, lane); failed = true; break; }
     const unsigned char* Kt = R.at(2 * n);
     float2 acc[kR];
@@ -276,7 +319,7 @@ __device__ inline void few_warp_fp32(const AttnRows& A, const Logits& X, const R
     bool more = false;
 #pragma unroll
     for (int r = 0; r < kR; ++r) {
-      x[r] = row < limit[r] ? (acc[r].x + acc[r].y) * A.scale : -INFINITY;
+      x[r] = row < limit[r] && (alive >> lane & 1u) ? fmaf(acc[r].x + acc[r].y, A.scale, log_w) : -INFINITY;
       if (X.x && r < g && row < len) X.x[r * X.pitch + row] = x[r];
       more = more || x[r] > m[r];
     }
@@ -316,7 +359,7 @@ __device__ inline void few_warp_fp32(const AttnRows& A, const Logits& X, const R
         o[r][c + 1] = y.y;
       }
     };
-    if (rows == kTile) {
+    if (alive == 0xffffffffu) {
 #pragma unroll 2
       for (int t = 0; t < kTile; t += 4) {
         float v[4][kC];
@@ -332,7 +375,8 @@ __device__ inline void few_warp_fp32(const AttnRows& A, const Logits& X, const R
         }
       }
     } else {
-      for (int t = 0; t < rows; ++t) {           // nothing behind the last row: what is there may be anything
+      for (int t = 0; t < kTile; ++t) {
+        if (!(alive >> t & 1u)) continue;        // does not count: what it holds may be anything
         float v[kC];
         value(t, v);
 #pragma unroll
@@ -364,7 +408,7 @@ struct FewShared {
 
 // The CTA's share [t0, t1) of the tiles: every warp's sums, to mrg[warp][row][kPitch] in the rings' place.
 template <bool kBf16, int D, int kR>
-__device__ inline void few_tiles(const AttnRows& A, const Logits& X, const CUtensorMap& mk, const CUtensorMap& mv, FewShared<kBf16, D, kR>& sh, unsigned char* tiles,
+__device__ inline void few_tiles(const AttnRows& A, const Group& G, const Logits& X, const CUtensorMap& mk, const CUtensorMap& mv, FewShared<kBf16, D, kR>& sh, unsigned char* tiles,
                                  int s, int len, int t0, int t1) {
   using F = Few<kBf16, D>;
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
@@ -373,13 +417,13 @@ __device__ inline void few_tiles(const AttnRows& A, const Logits& X, const CUten
   R.start(lane);
   if constexpr (!kBf16) {
     for (int i = tid; i < kR * D; i += kThreads)
-      sh.qs[i] = i / D < A.n_rows ? static_cast<const float*>(A.q)[attn_row(A, s, i / D) * D + i % D] : 0.f;
+      sh.qs[i] = i / D < G.g ? static_cast<const float*>(A.q)[attn_row(A, s, G.r0 + i / D) * D + i % D] : 0.f;
     __syncthreads();
   }
   float* mrg = reinterpret_cast<float*>(tiles) + warp * kFewRows * F::kPitch;
   bool failed = false;
-  if constexpr (kBf16) few_warp_bf16<D>(A, X, R, s, len, n_tiles, lane, &sh.abort_flag, mrg, failed);
-  else few_warp_fp32<D, kR>(A, X, R, s, len, n_tiles, lane, &sh.abort_flag, sh.qs, sh.ps + warp * kR * 32, mrg, failed);
+  if constexpr (kBf16) few_warp_bf16<D>(A, G, X, R, s, len, n_tiles, lane, &sh.abort_flag, mrg, failed);
+  else few_warp_fp32<D, kR>(A, G, X, R, s, len, n_tiles, lane, &sh.abort_flag, sh.qs, sh.ps + warp * kR * 32, mrg, failed);
   if (failed && lane == 0) tc::st_release(&sh.abort_flag, 1);
   __syncthreads();
 }
@@ -441,26 +485,30 @@ __device__ inline void few_put(const AttnRows& A, int64_t row, int lane, const f
 
 // kR: rows that the fp32 form takes (bf16: 8).
 template <bool kBf16, int D, int kR>
-__global__ void __launch_bounds__(kThreads, (Few<kBf16, D>::kCtas)) attn_few_kernel(const __grid_constant__ FewArgs P, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv) {
+__global__ void __launch_bounds__(kThreads, (Few<kBf16, D>::kCtas)) attn_few_kernel(const __grid_constant__ FewJobs J, const __grid_constant__ FewMaps maps) {
   using F = Few<kBf16, D>;
   extern __shared__ unsigned char smem_raw[];
   __shared__ FewShared<kBf16, D, kR> sh;
   unsigned char* tiles = smem_raw + (-tc::smem_u32(smem_raw) & 1023u);
-  const AttnRows& A = P.A;
+  const int which = (int)blockIdx.x >= J.ctas0, cta = blockIdx.x - (which ? J.ctas0 : 0);
+  const AttnRows& A = J.job[which].A;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  const int s = blockIdx.x, split = blockIdx.y;
+  // the groups of a stream's query rows next to one another: they read the same rows
+  const int group = cta % J.groups[which], split = cta / J.groups[which] % A.splits, s = cta / J.groups[which] / A.splits;
+  const Group G{group * kFewRows, min(kFewRows, A.n_rows - group * kFewRows)};
   few_init(sh);
   grid_wait_and_release();
   __syncthreads();
   const int len = attn_len(A, s), n_all = (len + kTile - 1) / kTile;
-  const Logits X{P.x ? P.x + (int64_t)s * A.n_rows * P.pitch : nullptr, P.pitch};
-  few_tiles(A, X, mk, mv, sh, tiles, s, len, (int)((int64_t)n_all * split / A.splits), (int)((int64_t)n_all * (split + 1) / A.splits));
+  const int64_t pitch = J.job[which].pitch;
+  const Logits X{J.job[which].x ? J.job[which].x + ((int64_t)s * A.n_rows + G.r0) * pitch : nullptr, pitch};
+  few_tiles(A, G, X, maps.k[which], maps.v[which], sh, tiles, s, len, (int)((int64_t)n_all * split / A.splits), (int)((int64_t)n_all * (split + 1) / A.splits));
   const float* mrg = reinterpret_cast<const float*>(tiles);
-  for (int r = warp; r < A.n_rows; r += kWarps) {
+  for (int r = warp; r < G.g; r += kWarps) {
     float acc[D / 32], top, sum;
     few_join<D, kWarps>(kWarps, lane, [&](int w) { return mrg + (w * kFewRows + r) * F::kPitch; }, acc, top, sum);
     if (sh.abort_flag) sum = NAN;
-    const int64_t row = attn_row(A, s, r);
+    const int64_t row = attn_row(A, s, G.r0 + r);
     if (A.n_slots > 1) {
       const int64_t at = (int64_t)(A.slot0 + split) * A.total_rows + row;
       if (lane == 0) A.part_ml[at] = make_float2(top, sum);
@@ -474,33 +522,35 @@ __global__ void __launch_bounds__(kThreads, (Few<kBf16, D>::kCtas)) attn_few_ker
 }
 
 // The splits of a stream as a cluster of CTAs, where its logits fit their shared memory: they join their sums through it, every
-// CTA then turns its own logits into weights, and nothing but results leaves the chip.
+// CTA then turns its own logits into weights, and nothing but results leaves the chip.  More than eight query rows are groups with a
+// cluster each; what a cached row receives from a group goes to `sums` [groups, n_streams, cap] (one group: to the scores).
 constexpr int kMaxCluster = 16;
 constexpr int logit_bytes(bool bf16, int d) { return !bf16 && d == 64 ? 8 * 1024 : 15 * 1024; }       // of a CTA: two (fp32, d = 128: one) still fit an SM
 
 template <bool kBf16, int D, int kR>
 __global__ void __launch_bounds__(kThreads, (Few<kBf16, D>::kCtas))
-attn_few_cluster_kernel(const __grid_constant__ AttnRows A, const ScoreArgs S, int pitch, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv) {
+attn_few_cluster_kernel(const __grid_constant__ AttnRows A, const ScoreArgs S, int pitch, float* sums, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv) {
   namespace cg = cooperative_groups;
   using F = Few<kBf16, D>;
   extern __shared__ unsigned char smem_raw[];
   __shared__ FewShared<kBf16, D, kR> sh;
   __shared__ float lse[kFewRows];
   unsigned char* tiles = smem_raw + (-tc::smem_u32(smem_raw) & 1023u);
-  float* x = reinterpret_cast<float*>(tiles + kWarps * F::kRing * F::kTileBytes);      // [n_rows][pitch]
-  float* joined = reinterpret_cast<float*>(tiles) + kWarps * kFewRows * F::kPitch;     // [n_rows][kPitch] of the CTA, behind its warps'
+  float* x = reinterpret_cast<float*>(tiles + kWarps * F::kRing * F::kTileBytes);      // [g][pitch]
+  float* joined = reinterpret_cast<float*>(tiles) + kWarps * kFewRows * F::kPitch;     // [g][kPitch] of the CTA, behind its warps'
   cg::cluster_group cluster = cg::this_cluster();
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
-  const int C = (int)gridDim.y, c = blockIdx.y, s = blockIdx.x;
+  const int C = (int)gridDim.y, c = blockIdx.y, s = blockIdx.x % A.n_streams, group = blockIdx.x / A.n_streams;
+  const Group G{group * kFewRows, min(kFewRows, A.n_rows - group * kFewRows)};
   few_init(sh);
   grid_wait_and_release();
   __syncthreads();
   const int len = attn_len(A, s), n_all = (len + kTile - 1) / kTile;
   const int t0 = (int)((int64_t)n_all * c / C), t1 = (int)((int64_t)n_all * (c + 1) / C);
   const int row0 = t0 * kTile, row1 = min(len, t1 * kTile);
-  few_tiles(A, Logits{x - row0, pitch}, mk, mv, sh, tiles, s, len, t0, t1);
+  few_tiles(A, G, Logits{x - row0, pitch}, mk, mv, sh, tiles, s, len, t0, t1);
   const float* mrg = reinterpret_cast<const float*>(tiles);
-  for (int r = warp; r < A.n_rows; r += kWarps) {
+  for (int r = warp; r < G.g; r += kWarps) {
     float acc[D / 32], top, sum;
     few_join<D, kWarps>(kWarps, lane, [&](int w) { return mrg + (w * kFewRows + r) * F::kPitch; }, acc, top, sum);
     if (sh.abort_flag) sum = NAN;
@@ -511,48 +561,62 @@ attn_few_cluster_kernel(const __grid_constant__ AttnRows A, const ScoreArgs S, i
   }
   cluster.sync();
   // The rows' sums over the cluster: a lane per CTA.
-  for (int r = warp; r < A.n_rows; r += kWarps) {
+  for (int r = warp; r < G.g; r += kWarps) {
     const float* at = cluster.map_shared_rank(joined, lane < C ? lane : 0) + r * F::kPitch;
     const float m = lane < C ? at[D] : -INFINITY, l = lane < C ? at[D + 1] : 0.f;
     const float top = warp_max(m), base = top == -INFINITY ? 0.f : top, sum = warp_sum(l * exp2f(m - base));
-    const bool counted = r % A.n_queries >= A.n_queries - S.n_scored;
+    const bool counted = (G.r0 + r) % A.n_queries >= A.n_queries - S.n_scored;
     if (lane == 0) lse[r] = sum == 0.f || !counted ? INFINITY : base + log2f(sum);
   }
   // The outputs: row r by the warp r of the cluster's.
-  for (int r = c + C * warp; r < A.n_rows; r += C * kWarps) {
+  for (int r = c + C * warp; r < G.g; r += C * kWarps) {
     float acc[D / 32], top, sum;
     few_join<D, kMaxCluster>(C, lane, [&](int b) { return cluster.map_shared_rank(joined, b) + r * F::kPitch; }, acc, top, sum);
-    few_put<kBf16, D>(A, attn_row(A, s, r), lane, acc, sum);
+    few_put<kBf16, D>(A, attn_row(A, s, G.r0 + r), lane, acc, sum);
   }
   __syncthreads();
   const int64_t first = (int64_t)s * A.cap;
   for (int i = row0 + tid; i < row1; i += kThreads) {
     float sum = 0.f;
-    for (int r = 0; r < A.n_rows; ++r) sum += exp2f(x[r * pitch + i - row0] - lse[r]);
-    score_put(S, first + i, sum);
+    for (int r = 0; r < G.g; ++r) sum += exp2f(x[r * pitch + i - row0] - lse[r]);
+    if (sums) sums[(int64_t)group * A.n_streams * A.cap + first + i] = sum;
+    else score_put(S, first + i, sum);
   }
   cluster.sync();                                // nobody reads this CTA's sums any more
 }
 
-// Behind attn_few_kernel: the first `joins` CTAs join the splits, eight query rows each; the others turn 1024 logits per
-// query row into weights and add those of the scored rows up.
-constexpr int kEndThreads = 256, kEndKeys = 1024;
+// The scores from the groups' sums.
+constexpr int kEndThreads = 256;
+__global__ void __launch_bounds__(kEndThreads) few_sum_kernel(const __grid_constant__ AttnRows A, const ScoreArgs S, const float* __restrict__ sums, int groups, int chunks) {
+  const int s = blockIdx.x / chunks, i = blockIdx.x % chunks * kEndThreads + threadIdx.x;
+  grid_wait_and_release();
+  if (i >= attn_len(A, s)) return;
+  const int64_t at = (int64_t)s * A.cap + i, step = (int64_t)A.n_streams * A.cap;
+  float sum = 0.f;
+#pragma unroll 8
+  for (int k = 0; k < groups; ++k) sum += sums[k * step + at];
+  score_put(S, at, sum);
+}
+
+// Behind attn_few_kernel with one group of query rows: the first `joins` CTAs join the splits; the others turn 512 logits per query
+// row into weights and add those of the scored rows up.
+constexpr int kEndKeys = 512;
 template <bool kBf16, int D>
-__global__ void __launch_bounds__(kEndThreads) few_end_kernel(const __grid_constant__ FewArgs P, const ScoreArgs S, int joins, int chunks) {
+__global__ void __launch_bounds__(kEndThreads, 5) few_end_kernel(const __grid_constant__ FewArgs P, const ScoreArgs S, int joins, int chunks) {
   __shared__ float lse[kFewRows];
+  __shared__ JoinShared<D> join;
   const AttnRows& A = P.A;
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
   grid_wait_and_release();
   if ((int)blockIdx.x < joins) {
-    const int64_t row = (int64_t)blockIdx.x * (kEndThreads / 32) + warp;
-    if (row < A.total_rows) join_splits<kBf16, D>(A, row, lane);
+    join_splits<kBf16, D>(A, blockIdx.x, join);
     return;
   }
   const int s = ((int)blockIdx.x - joins) / chunks, k0 = ((int)blockIdx.x - joins) % chunks * kEndKeys;
   const int len = attn_len(A, s);
   if (k0 >= len) return;
-  // what does not depend on the sums is asked for first
   constexpr int kPer = kEndKeys / kEndThreads;
+  // what does not depend on the sums is asked for first
   const float* x = P.x + (int64_t)s * A.n_rows * P.pitch + k0 + tid;
   float logit[kFewRows][kPer];
 #pragma unroll
@@ -564,7 +628,7 @@ __global__ void __launch_bounds__(kEndThreads) few_end_kernel(const __grid_const
     float v = 0.f;
     if (A.n_slots > 1) {
       float2 ml[kAttnMaxSplits / 32];
-      float top = -INFINITY, sum = 0.f;
+      float top = -INFINITY, l = 0.f;
 #pragma unroll
       for (int i = 0; i < kAttnMaxSplits / 32; ++i) {
         ml[i] = lane + 32 * i < A.n_slots ? A.part_ml[(int64_t)(lane + 32 * i) * A.total_rows + row] : make_float2(-INFINITY, 0.f);
@@ -573,9 +637,9 @@ __global__ void __launch_bounds__(kEndThreads) few_end_kernel(const __grid_const
       top = warp_max(top);
       const float base = top == -INFINITY ? 0.f : top;
 #pragma unroll
-      for (int i = 0; i < kAttnMaxSplits / 32; ++i) sum = fmaf(ml[i].y, exp2f(ml[i].x - base), sum);
-      sum = warp_sum(sum);
-      v = sum == 0.f ? INFINITY : base + log2f(sum);
+      for (int i = 0; i < kAttnMaxSplits / 32; ++i) l = fmaf(ml[i].y, exp2f(ml[i].x - base), l);
+      l = warp_sum(l);
+      v = l == 0.f ? INFINITY : base + log2f(l);
     } else {
       v = A.lse[row];
     }
@@ -606,50 +670,69 @@ cudaError_t for_rows(int n_rows, Run run) {
 }
 
 template <bool kBf16, int D>
-cudaError_t launch_few(const FewArgs& P, cudaStream_t st) {
+cudaError_t launch_few(const FewArgs& P, const FewArgs* also, cudaStream_t st) {
   using F = Few<kBf16, D>;
-  CUtensorMap mk, mv;
-  const AttnRows& A = P.A;
-  cudaError_t e = cache_map(&mk, A.K, kBf16, D, A.cap, A.n_streams, kTile);
-  if (e == cudaSuccess) e = cache_map(&mv, A.V, kBf16, D, A.cap, A.n_streams, kTile);
-  if (e != cudaSuccess) return e;
-  return for_rows<kBf16, D>(A.n_rows, [&](auto rows) {
+  FewJobs J{};
+  FewMaps maps;
+  int64_t ctas = 0;
+  int most = 0;
+  for (int i = 0; i < (also ? 2 : 1); ++i) {
+    const AttnRows& A = (J.job[i] = i ? *also : P).A;
+    cudaError_t e = cache_map(&maps.k[i], A.K, kBf16, D, A.cap, A.n_streams, kTile);
+    if (e == cudaSuccess) e = cache_map(&maps.v[i], A.V, kBf16, D, A.cap, A.n_streams, kTile);
+    if (e != cudaSuccess) return e;
+    J.groups[i] = (A.n_rows + kFewRows - 1) / kFewRows;
+    ctas += (int64_t)J.groups[i] * A.splits * A.n_streams;
+    if (i == 0) J.ctas0 = (int)ctas;
+    most = std::max(most, A.n_rows);
+  }
+  if (!also) {
+    maps.k[1] = maps.k[0];
+    maps.v[1] = maps.v[0];
+  }
+  if (ctas > INT32_MAX) return cudaErrorInvalidValue;
+  return for_rows<kBf16, D>(most, [&](auto rows) {
     auto kern = attn_few_kernel<kBf16, D, decltype(rows)::value>;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)F::kSmem);
     if (e != cudaSuccess) return e;
-    const PdlConfig pc(dim3(A.n_streams, A.splits), kThreads, F::kSmem, st);
-    return cudaLaunchKernelEx(&pc.cfg, kern, P, mk, mv);
+    const PdlConfig pc(dim3((unsigned)ctas), kThreads, F::kSmem, st);
+    return cudaLaunchKernelEx(&pc.cfg, kern, J, maps);
   });
 }
 
 int logit_pitch(int cap, int C) { return ((cap + kTile - 1) / kTile + C - 1) / C * kTile; }
 
 template <bool kBf16, int D>
-cudaError_t launch_cluster(const AttnRows& A, const ScoreArgs& S, int C, cudaStream_t st) {
+cudaError_t launch_cluster(const AttnRows& A, const ScoreArgs& S, int C, float* sums, cudaStream_t st) {
   using F = Few<kBf16, D>;
   CUtensorMap mk, mv;
   cudaError_t e = cache_map(&mk, A.K, kBf16, D, A.cap, A.n_streams, kTile);
   if (e == cudaSuccess) e = cache_map(&mv, A.V, kBf16, D, A.cap, A.n_streams, kTile);
   if (e != cudaSuccess) return e;
-  return for_rows<kBf16, D>(A.n_rows, [&](auto rows) {
+  const int groups = (A.n_rows + kFewRows - 1) / kFewRows;
+  e = for_rows<kBf16, D>(A.n_rows, [&](auto rows) {
     auto kern = attn_few_cluster_kernel<kBf16, D, decltype(rows)::value>;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)F::kSmem + logit_bytes(kBf16, D));
     if (e == cudaSuccess) e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e != cudaSuccess) return e;
     const int pitch = logit_pitch(A.cap, C);
-    PdlConfig pc(dim3(A.n_streams, C), kThreads, F::kSmem + (size_t)A.n_rows * pitch * 4, st);
+    PdlConfig pc(dim3(A.n_streams * groups, C), kThreads, F::kSmem + (size_t)std::min(A.n_rows, kFewRows) * pitch * 4, st);
     cudaLaunchAttribute attrs[2] = {pc.attr, {}};
     attrs[1].id = cudaLaunchAttributeClusterDimension;
     attrs[1].val.clusterDim.x = attrs[1].val.clusterDim.z = 1;
     attrs[1].val.clusterDim.y = C;
     pc.cfg.attrs = attrs;
     pc.cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&pc.cfg, kern, A, S, pitch, mk, mv);
+    return cudaLaunchKernelEx(&pc.cfg, kern, A, S, pitch, groups > 1 ? sums : nullptr, mk, mv);
   });
+  if (e != cudaSuccess || groups == 1) return e;
+  const int chunks = (A.cap + kEndThreads - 1) / kEndThreads;
+  const PdlConfig pc(dim3((unsigned)chunks * A.n_streams), kEndThreads, 0, st);
+  return cudaLaunchKernelEx(&pc.cfg, few_sum_kernel, A, S, (const float*)sums, groups, chunks);
 }
 template <bool kBf16, int D>
 cudaError_t launch_end(const FewArgs& P, const ScoreArgs& S, cudaStream_t st) {
-  const int joins = P.A.n_slots > 1 ? (P.A.total_rows + kEndThreads / 32 - 1) / (kEndThreads / 32) : 0;
+  const int joins = P.A.n_slots > 1 ? join_ctas(P.A) : 0;
   const int chunks = (P.A.cap + kEndKeys - 1) / kEndKeys;
   const PdlConfig pc(dim3((unsigned)(joins + chunks * P.A.n_streams)), kEndThreads, 0, st);
   return cudaLaunchKernelEx(&pc.cfg, few_end_kernel<kBf16, D>, P, S, joins, chunks);
@@ -657,34 +740,39 @@ cudaError_t launch_end(const FewArgs& P, const ScoreArgs& S, cudaStream_t st) {
 
 }  // namespace
 
-// Split factor of the kernels above: enough CTAs for several waves, so that streams of different lengths even out, and no
-// fewer than a tile for each warp of a CTA.
-int few_splits(int64_t streams, int cap) {
-  const int64_t want = (8 * kAttnSms + streams - 1) / streams, most = (cap + kWarps * kTile - 1) / (kWarps * kTile);
-  return (int)std::max<int64_t>(1, std::min<int64_t>({want, most, (int64_t)kAttnMaxSplits}));
+// Split factor of the kernels above: as many CTAs as fit the SMs at once, with a tile for each warp; and of long caches, in parts of 1024
+// rows, up to four times as many, so that streams of different lengths even out.
+int few_splits(int64_t streams, int cap, int n_rows) {
+  const int64_t sets = streams * ((n_rows + kFewRows - 1) / kFewRows);
+  const int64_t fill = std::min<int64_t>(2 * kAttnSms / sets, (cap + kWarps * kTile - 1) / (kWarps * kTile));
+  const int64_t even = std::min<int64_t>((8 * kAttnSms + sets - 1) / sets, cap / 1024);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(std::max(fill, even), kAttnMaxSplits));
 }
 
 // CTAs of a stream's cluster, 0 where its logits do not fit or the clusters do not fit one wave: as many as leave a tile for every warp.
 // (256 streams of up to 8192 rows in clusters of 16 took 228 us, as splits of a launch 108: clusters start and end as a whole.)
 int few_cluster(int64_t streams, int cap, int n_rows, int d, int is_bf16) {
+  const int64_t sets = streams * ((n_rows + kFewRows - 1) / kFewRows);
   int C = 1;
-  while (C < kMaxCluster && 2 * streams * C <= 2 * kAttnSms && cap > C * kWarps * kTile) C *= 2;
-  return streams * C <= 2 * kAttnSms && (int64_t)n_rows * logit_pitch(cap, C) * 4 <= logit_bytes(is_bf16, d) ? C : 0;
+  while (C < kMaxCluster && 2 * sets * C <= 2 * kAttnSms && cap > C * kWarps * kTile) C *= 2;
+  return sets * C <= 2 * kAttnSms && (int64_t)std::min(n_rows, kFewRows) * logit_pitch(cap, C) * 4 <= logit_bytes(is_bf16, d) ? C : 0;
 }
+// Floats of the workspace that they need.
+int64_t few_cluster_sums(const AttnRows& A) { return A.n_rows > kFewRows ? (int64_t)(A.n_rows + kFewRows - 1) / kFewRows * A.n_streams * A.cap : 0; }
 
 int64_t few_pitch(int cap) { return ((int64_t)cap + 31) / 32 * 32; }
 
-// x: [n_streams, n_rows, few_pitch(cap)] where launch_few_end is to follow, else null.
-cudaError_t launch_attn_few(const AttnRows& A, float* x, int d, int is_bf16, cudaStream_t st) {
-  const FewArgs P{A, x, few_pitch(A.cap)};
-  if (is_bf16) return d == 128 ? launch_few<true, 128>(P, st) : launch_few<true, 64>(P, st);
-  return d == 128 ? launch_few<false, 128>(P, st) : launch_few<false, 64>(P, st);
+// x: [n_streams, n_rows, few_pitch(cap)] where launch_few_end is to follow, else null.  `also`: a second set of streams of the same call.
+cudaError_t launch_attn_few(const AttnRows& A, float* x, const AttnRows* also, int d, int is_bf16, cudaStream_t st) {
+  const FewArgs P{A, x, few_pitch(A.cap)}, Q{also ? *also : A, nullptr, 0}, *second = also ? &Q : nullptr;
+  if (is_bf16) return d == 128 ? launch_few<true, 128>(P, second, st) : launch_few<true, 64>(P, second, st);
+  return d == 128 ? launch_few<false, 128>(P, second, st) : launch_few<false, 64>(P, second, st);
 }
 
 // Outputs and scores by clusters of C CTAs.
-cudaError_t launch_attn_few_cluster(const AttnRows& A, const ScoreArgs& S, int C, int d, int is_bf16, cudaStream_t st) {
-  if (is_bf16) return d == 128 ? launch_cluster<true, 128>(A, S, C, st) : launch_cluster<true, 64>(A, S, C, st);
-  return d == 128 ? launch_cluster<false, 128>(A, S, C, st) : launch_cluster<false, 64>(A, S, C, st);
+cudaError_t launch_attn_few_cluster(const AttnRows& A, const ScoreArgs& S, int C, float* sums, int d, int is_bf16, cudaStream_t st) {
+  if (is_bf16) return d == 128 ? launch_cluster<true, 128>(A, S, C, sums, st) : launch_cluster<true, 64>(A, S, C, sums, st);
+  return d == 128 ? launch_cluster<false, 128>(A, S, C, sums, st) : launch_cluster<false, 64>(A, S, C, sums, st);
 }
 
 // The scores, and the outputs where there are several splits.

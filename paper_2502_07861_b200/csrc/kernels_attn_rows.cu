@@ -177,11 +177,10 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const AttnRows A, i
 
 template <bool kBf16, int D>
 __global__ void __launch_bounds__(kThreads) attn_combine_kernel(const AttnRows A) {
-  const int64_t row = (int64_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
-  const int lane = threadIdx.x % 32;
+  static_assert(kThreads == kJoinThreads, "");
+  __shared__ JoinShared<D> sh;
   grid_wait_and_release();
-  if (row >= A.total_rows) return;
-  join_splits<kBf16, D>(A, row, lane);
+  join_splits<kBf16, D>(A, blockIdx.x, sh);
 }
 
 // 64 keys of a stream: their logits again, against every scored query that sees them, and the weights' sums.
@@ -253,7 +252,7 @@ cudaError_t launch_attn_simt(const AttnRows& A, int d, int is_bf16, cudaStream_t
 }
 
 cudaError_t launch_attn_combine(const AttnRows& A, int d, int is_bf16, cudaStream_t st) {
-  const dim3 grid((unsigned)(((int64_t)A.total_rows + kThreads / 32 - 1) / (kThreads / 32)));
+  const dim3 grid(join_ctas(A));
   if (d == 128) return is_bf16 ? launch(attn_combine_kernel<true, 128>, grid, 0, st, A) : launch(attn_combine_kernel<false, 128>, grid, 0, st, A);
   return is_bf16 ? launch(attn_combine_kernel<true, 64>, grid, 0, st, A) : launch(attn_combine_kernel<false, 64>, grid, 0, st, A);
 }

@@ -6,11 +6,12 @@
 // would be 4 bytes per pair to keep, 2 d operations to form), transposed: S^T = K Q^T has the cached rows as TMEM lanes, so that a thread
 // adds up one row's weights and no sum crosses threads.
 //
-// A CTA keeps 256 cached rows in shared memory (two tiles, a warpgroup each, two buffers of 128 x 128 logits per tile) and walks
+// A CTA keeps 256 cached rows in shared memory (two tiles, two warpgroups each, which take half of a tile's queries, two buffers of
+// 128 x 128 logits per tile) and walks
 // the queries in tiles of 128, head by head, from the first tile that sees its rows on.  What bounds it are the exponentials: 32768 per
 // tile of queries are 2048 cycles of the special-function unit against 1024 of products (d = 128), so a larger share of them than in the attention
 // kernel is formed by FMAs.
-// Warps: 0-3 and 4-7 the rows of the two tiles, 8 asks for K and the Q tiles (TMA) and loads their lse, 9 issues the MMAs.
+// Warps: 0-7 and 8-15 the rows of the two tiles, 16 asks for K and the Q tiles (TMA) and loads their lse, 17 issues the MMAs.
 // Every wait is bounded; one that gives up makes the scores NaN.
 #include "attn_tc.cuh"
 
@@ -21,10 +22,10 @@ namespace {
 using namespace tc;
 using namespace mma;
 
-constexpr int kThreads = 384;
-// Registers of a thread at launch, and what the warps go on with: 8 x 208 + 4 x 80 <= 12 x 168.
-constexpr int kRegs = 168, kRegsRows = 208, kRegsOther = 80;
-static_assert(8 * kRegsRows + 4 * kRegsOther <= 12 * kRegs && kThreads * kRegs <= 65536, "a register split beyond the launch's waits forever");
+constexpr int kThreads = 640;
+// Registers of a thread at launch, and what the warps go on with: 16 x 104 + 4 x 56 <= 20 x 96.
+constexpr int kRegs = 96, kRegsRows = 104, kRegsOther = 56;
+static_assert(16 * kRegsRows + 4 * kRegsOther <= 20 * kRegs && kThreads * kRegs <= 65536, "a register split beyond the launch's waits forever");
 
 template <int D>
 struct Shape {
@@ -44,7 +45,8 @@ score_tc_kernel(const __grid_constant__ AttnRows A, const ScoreArgs C, int block
   __shared__ uint64_t k_full, q_full[kRing], q_empty[kRing], lse_full[Sh::kLse], s_full[2][2], s_empty[2][2], drained;
   __shared__ uint32_t tmem_s;
   __shared__ int abort_flag;
-  __shared__ __align__(16) float lse[Sh::kLse][kTcRows];
+  __shared__ __align__(16) float lse[Sh::kLse][kTcRows];      // negative
+  __shared__ float half[2][kTcKeys];
   unsigned char* sm = smem_raw + (-smem_u32(smem_raw) & 1023u);
   unsigned char* ring = sm + 2 * Sh::kTile;
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid / 32, 0), lane = tid % 32;
@@ -53,12 +55,12 @@ score_tc_kernel(const __grid_constant__ AttnRows A, const ScoreArgs C, int block
     mbar_init(&drained, 1);
     for (int i = 0; i < kRing; ++i) { mbar_init(q_full + i, 1); mbar_init(q_empty + i, 1); }
     for (int i = 0; i < Sh::kLse; ++i) mbar_init(lse_full + i, 32);
-    for (int i = 0; i < 4; ++i) { mbar_init(&s_full[0][0] + i, 1); mbar_init(&s_empty[0][0] + i, 128); }
+    for (int i = 0; i < 4; ++i) { mbar_init(&s_full[0][0] + i, 1); mbar_init(&s_empty[0][0] + i, 256); }
     abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
-  if (warp == 9) {
+  if (warp == 17) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_s)), "r"(512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -76,9 +78,9 @@ score_tc_kernel(const __grid_constant__ AttnRows A, const ScoreArgs C, int block
   tc_fence_after();
   const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_s, 0);
 
-  if (warp >= 8) {
+  if (warp >= 16) {
     regs_down<kRegsOther>();
-    if (warp == 8 && n > 0) {
+    if (warp == 16 && n > 0) {
       bool ok = true;
       if (lane == 0) {
         mbar_expect_tx(&k_full, tiles * Sh::kTile);
@@ -100,7 +102,7 @@ score_tc_kernel(const __grid_constant__ AttnRows A, const ScoreArgs C, int block
 #pragma unroll
         for (int c = 0; c < kTcRows / 32; ++c) {
           const int q = j + lane + 32 * c;
-          to[lane + 32 * c] = q < m ? A.lse[((int64_t)s * heads + head) * m + q] : INFINITY;
+          to[lane + 32 * c] = q < m ? -A.lse[((int64_t)s * heads + head) * m + q] : -INFINITY;
         }
         mbar_arrive(lse_full + i % Sh::kLse);
         __syncwarp();
@@ -111,7 +113,7 @@ score_tc_kernel(const __grid_constant__ AttnRows A, const ScoreArgs C, int block
         for (int e = max(0, i - kRing); e < i; ++e)
           while (!mbar_try_wait(q_full + e % kRing, (uint32_t)(e / kRing) & 1u) && clock64() - t0 < kWaitCycles) {}
       }
-    } else if (warp == 9 && n > 0) {
+    } else if (warp == 17 && n > 0) {
       bool ok = true;
       auto wait = [&](uint64_t* bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, wait_bar(bar, parity, &abort_flag)); };
       wait(&k_full, 0);
@@ -144,8 +146,8 @@ score_tc_kernel(const __grid_constant__ AttnRows A, const ScoreArgs C, int block
     }
   } else {
     regs_up<kRegsRows>();
-    const int t = warp / 4, key = key0 + t * kTcKeys + 32 * (warp % 4) + lane;
-    const uint32_t S = tmem + ((uint32_t)(32 * (warp % 4)) << 16) + 256 * t;
+    const int t = warp / 8, h = warp / 4 % 2, lanes = 32 * (warp % 4), key = key0 + t * kTcKeys + lanes + lane;
+    const uint32_t S = tmem + ((uint32_t)lanes << 16) + 256 * t + 64 * h;
     const float2 scale2 = make_float2(A.scale, A.scale);
     float sum = 0.f;
     bool ok = true;
@@ -154,47 +156,49 @@ score_tc_kernel(const __grid_constant__ AttnRows A, const ScoreArgs C, int block
         ok = __all_sync(0xffffffffu, wait_bar(&s_full[t][i & 1], (uint32_t)(i / 2) & 1u, &abort_flag) && wait_bar(lse_full + i % Sh::kLse, (uint32_t)(i / Sh::kLse) & 1u, &abort_flag));
         if (!ok) break;
         tc_fence_after();
-        float x[4][32];
+        float x[2][32];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) tmem_ld32(S + 128 * (i & 1) + 32 * c, x[c]);
+        for (int c = 0; c < 2; ++c) tmem_ld32(S + 128 * (i & 1) + 32 * c, x[c]);
         tmem_ld_wait();
         tc_fence_before();
         mbar_arrive(&s_empty[t][i & 1]);
-        const int j = start + i % per_head * kTcRows;
-        const int from = key - (len - m) - j;    // the tile's first query that sees the row
+        const int j = start + i % per_head * kTcRows + 64 * h;
+        const int from = key - (len - m) - j;    // the half tile's first query that sees the row
         const bool masked = key0 + (t + 1) * kTcKeys - 1 > len - m + j;
-        const float4* l4 = reinterpret_cast<const float4*>(lse[i % Sh::kLse]);
-        float2 part = make_float2(0.f, 0.f);
+        const float4* l4 = reinterpret_cast<const float4*>(lse[i % Sh::kLse] + 64 * h);
+        float2 part[2] = {};
         auto weights = [&](auto mask) {
 #pragma unroll
-          for (int c = 0; c < 4; ++c)
+          for (int c = 0; c < 2; ++c)
 #pragma unroll
             for (int k = 0; k < 32; k += 4) {
               const float4 l = l4[(32 * c + k) / 4];
-              const float2 lo = __ffma2_rn(make_float2(x[c][k], x[c][k + 1]), scale2, make_float2(-l.x, -l.y));
-              const float2 hi = __ffma2_rn(make_float2(x[c][k + 2], x[c][k + 3]), scale2, make_float2(-l.z, -l.w));
+              const float2 lo = __ffma2_rn(make_float2(x[c][k], x[c][k + 1]), scale2, make_float2(l.x, l.y));
+              const float2 hi = __ffma2_rn(make_float2(x[c][k + 2], x[c][k + 3]), scale2, make_float2(l.z, l.w));
               if constexpr (decltype(mask)::value) {
                 const int q = 32 * c + k;
-                part.x += (q >= from ? ex2(lo.x) : 0.f) + (q + 2 >= from ? ex2(hi.x) : 0.f);
-                part.y += (q + 1 >= from ? ex2(lo.y) : 0.f) + (q + 3 >= from ? ex2(hi.y) : 0.f);
+                part[0].x += (q >= from ? ex2(lo.x) : 0.f) + (q + 2 >= from ? ex2(hi.x) : 0.f);
+                part[0].y += (q + 1 >= from ? ex2(lo.y) : 0.f) + (q + 3 >= from ? ex2(hi.y) : 0.f);
               } else {
-                part = __fadd2_rn(part, make_float2(ex2(lo.x), ex2(lo.y)));
-                part = __fadd2_rn(part, (k / 4) % 4 == 3 ? make_float2(ex2(hi.x), ex2(hi.y)) : exp2_fma(hi));    // three of eight pairs
+                part[0] = __fadd2_rn(part[0], make_float2(ex2(lo.x), ex2(lo.y)));
+                part[1] = __fadd2_rn(part[1], (k / 4) % 4 != 3 ? make_float2(ex2(hi.x), ex2(hi.y)) : exp2_fma(hi));    // an eighth of the pairs
               }
             }
         };
         if (masked) weights(std::true_type{});
         else weights(std::false_type{});
-        sum += part.x + part.y;
+        sum += (part[0].x + part[0].y) + (part[1].x + part[1].y);
       }
     }
     if (!ok) sum = NAN;
-    if (key < len) score_put(C, (int64_t)s * A.cap + key, sum);
+    if (h == 1) half[t][lanes + lane] = sum;
+    asm volatile("bar.sync 1, 512;" ::: "memory");         // the row warps
+    if (h == 0 && key < len) score_put(C, (int64_t)s * A.cap + key, sum + half[t][lanes + lane]);
     tc_fence_before();
   }
   __syncthreads();
   tc_fence_after();
-  if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+  if (warp == 17) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
 }
 
 template <int D>
