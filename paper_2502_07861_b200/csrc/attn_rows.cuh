@@ -51,9 +51,9 @@ struct ScoreArgs {
   float decay;
   int32_t n_scored;
 };
-__device__ inline void score_put(const ScoreArgs& S, int64_t at, float sum) {
-  S.out[at] = S.in ? fmaf(S.decay, S.in[at], sum) : sum;
-}
+__device__ inline float score_old(const ScoreArgs& S, int64_t at) { return S.in ? S.in[at] : 0.f; }
+__device__ inline void score_put(const ScoreArgs& S, int64_t at, float old, float sum) { S.out[at] = S.in ? fmaf(S.decay, old, sum) : sum; }
+__device__ inline void score_put(const ScoreArgs& S, int64_t at, float sum) { score_put(S, at, score_old(S, at), sum); }
 
 // Joining the slots of query rows: their sums brought to one maximum and added.  A CTA of eight warps takes eight rows, or, of more than
 // eight slots, two rows with four warps each, which add every fourth slot up and then one another's sums: the order depends on sizes alone.
@@ -64,9 +64,10 @@ template <int D>
 struct JoinShared {
   float acc[kJoinThreads / 32][D];
 };
-template <bool kBf16, int D>
+// kAhead: slots that a warp asks for at once.
+template <bool kBf16, int D, int kAhead>
 __device__ inline void join_splits(const AttnRows& A, int cta, JoinShared<D>& sh) {
-  constexpr int kPer = D / 32, kChunks = kJoinMaxSlots / 32, kAhead = 8;
+  constexpr int kPer = D / 32, kChunks = kJoinMaxSlots / 32;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, rows = join_rows(A), ways = kJoinThreads / 32 / rows, way = warp % ways;
   const int64_t row = (int64_t)cta * rows + warp / ways;
   const bool held = row < A.total_rows;

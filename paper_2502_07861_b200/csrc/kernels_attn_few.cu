@@ -602,14 +602,14 @@ __global__ void __launch_bounds__(kEndThreads) few_sum_kernel(const __grid_const
 // row into weights and add those of the scored rows up.
 constexpr int kEndKeys = 512;
 template <bool kBf16, int D>
-__global__ void __launch_bounds__(kEndThreads, 5) few_end_kernel(const __grid_constant__ FewArgs P, const ScoreArgs S, int joins, int chunks) {
+__global__ void __launch_bounds__(kEndThreads, 6) few_end_kernel(const __grid_constant__ FewArgs P, const ScoreArgs S, int joins, int chunks) {
   __shared__ float lse[kFewRows];
   __shared__ JoinShared<D> join;
   const AttnRows& A = P.A;
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
   grid_wait_and_release();
   if ((int)blockIdx.x < joins) {
-    join_splits<kBf16, D>(A, blockIdx.x, join);
+    join_splits<kBf16, D, 2>(A, blockIdx.x, join);
     return;
   }
   const int s = ((int)blockIdx.x - joins) / chunks, k0 = ((int)blockIdx.x - joins) % chunks * kEndKeys;
@@ -618,7 +618,9 @@ __global__ void __launch_bounds__(kEndThreads, 5) few_end_kernel(const __grid_co
   constexpr int kPer = kEndKeys / kEndThreads;
   // what does not depend on the sums is asked for first
   const float* x = P.x + (int64_t)s * A.n_rows * P.pitch + k0 + tid;
-  float logit[kFewRows][kPer];
+  float logit[kFewRows][kPer], old[kPer];
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) old[j] = k0 + tid + j * kEndThreads < len ? score_old(S, (int64_t)s * A.cap + k0 + tid + j * kEndThreads) : 0.f;
 #pragma unroll
   for (int r = 0; r < kFewRows; ++r)
 #pragma unroll
@@ -658,7 +660,7 @@ __global__ void __launch_bounds__(kEndThreads, 5) few_end_kernel(const __grid_co
 #pragma unroll
   for (int j = 0; j < kPer; ++j) {
     const int key = k0 + tid + j * kEndThreads;
-    if (key < len) score_put(S, (int64_t)s * A.cap + key, sum[j]);
+    if (key < len) score_put(S, (int64_t)s * A.cap + key, old[j], sum[j]);
   }
 }
 

@@ -180,7 +180,7 @@ __global__ void __launch_bounds__(kThreads) attn_combine_kernel(const AttnRows A
   static_assert(kThreads == kJoinThreads, "");
   __shared__ JoinShared<D> sh;
   grid_wait_and_release();
-  join_splits<kBf16, D>(A, blockIdx.x, sh);
+  join_splits<kBf16, D, 8>(A, blockIdx.x, sh);
 }
 
 // 64 keys of a stream: their logits again, against every scored query that sees them, and the weights' sums.

@@ -18,7 +18,8 @@ namespace cg = cooperative_groups;
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kPasses = 3, kBins = 2048;
 constexpr int kMaxCluster = 8;
-constexpr int kStageRows = 49152;              // keys that a CTA keeps in shared memory; of longer slices they are formed anew
+constexpr int kStageRows = 24576;              // rows whose keys and positions a CTA keeps in shared memory; those of longer slices are read again
+constexpr int kAhead = 4;                      // rows that a thread asks for at once
 
 constexpr uint32_t kSafe = 0xffffffffu;
 
@@ -29,15 +30,61 @@ __device__ inline uint32_t score_key(float x) {
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
+struct SelectShared {
+  __align__(16) uint32_t hist[kPasses][kBins];
+  uint32_t coarse[kPasses][kBins / 64];          // sums of 64 bins
+  int warp_a[kWarps], warp_b[kWarps];
+  int cta[3][2];                                 // what the cluster's CTAs tell one another, a place per exchange
+  int before_a, before_b, all_a;                 // of the CTAs before this one; of all
+  int digit, above;
+  unsigned long long warp_least[kWarps], cta_least;
+};
+
+// Sums of a and b over the warps (a value per warp, by lane 0) and the cluster's CTAs: what lies before the warp, and all.  For all threads.
+__device__ inline void sums_before(cg::cluster_group& cluster, SelectShared& sh, int place, int C, int c, int& a, int& b, int& all) {
+  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+  if (lane == 0) { sh.warp_a[warp] = a; sh.warp_b[warp] = b; }
+  __syncthreads();
+  if (warp == 0) {
+    const int x = __reduce_add_sync(0xffffffffu, lane < kWarps ? sh.warp_a[lane] : 0), y = __reduce_add_sync(0xffffffffu, lane < kWarps ? sh.warp_b[lane] : 0);
+    if (lane == 0) { sh.cta[place][0] = x; sh.cta[place][1] = y; }
+  }
+  cluster.sync();
+  if (warp == 0) {
+    const int* far = lane < C ? cluster.map_shared_rank(&sh.cta[place][0], lane) : nullptr;
+    const int x = far ? far[0] : 0, y = far ? far[1] : 0;
+    const int bx = __reduce_add_sync(0xffffffffu, lane < c ? x : 0), by = __reduce_add_sync(0xffffffffu, lane < c ? y : 0), ax = __reduce_add_sync(0xffffffffu, x);
+    if (lane == 0) { sh.before_a = bx; sh.before_b = by; sh.all_a = ax; }
+  }
+  __syncthreads();
+  a = sh.before_a;
+  b = sh.before_b;
+  all = sh.all_a;
+  for (int w = 0; w < warp; ++w) { a += sh.warp_a[w]; b += sh.warp_b[w]; }
+  __syncthreads();                               // the next sums may go there
+}
+
+// The lane whose share of the values n, the first lane's first, holds the need-th, and the sum before it.
+__device__ inline int lane_of(int n, int need, int& before) {
+  int incl = n;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int x = __shfl_up_sync(0xffffffffu, incl, o);
+    if ((threadIdx.x & 31) >= o) incl += x;
+  }
+  const uint32_t reached = __ballot_sync(0xffffffffu, incl >= need);
+  const int at = __ffs(reached) - 1;
+  before = __shfl_sync(0xffffffffu, incl - n, at);
+  return at;
+}
+
 __global__ void __launch_bounds__(kThreads) evict_select_kernel(const EvictArgs E, int per, int staged) {
-  extern __shared__ uint32_t keys[];
-  __shared__ __align__(16) uint32_t hist[kPasses][kBins];
-  __shared__ int warp_n[kWarps], warp_m[kWarps], scan[kWarps];
-  __shared__ int cta_newest, cta_eq, cta_holes, cta_movers, found, above;
+  extern __shared__ uint32_t keys[];             // [per], behind them the positions (E.pos) [per]
+  __shared__ SelectShared sh;
   cg::cluster_group cluster = cg::this_cluster();
   const int C = (int)cluster.num_blocks(), c = (int)cluster.block_rank();
   const int s = blockIdx.x / C, tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
-  for (int i = tid; i < kPasses * kBins; i += kThreads) (&hist[0][0])[i] = 0;
+  for (int i = tid; i < kPasses * kBins / 4; i += kThreads) reinterpret_cast<uint4*>(&sh.hist[0][0])[i] = make_uint4(0, 0, 0, 0);
   grid_wait_and_release();
   const int len = E.lens ? max(0, min(E.lens[s], E.cap)) : E.cap, k = min(len, E.keep);
   const int64_t first = (int64_t)s * E.cap;
@@ -55,26 +102,101 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const EvictArgs 
     return;
   }
   const int begin = min(len, c * per), end = min(len, begin + per);
-  int newest = len - 1;
-  if (E.pos && E.n_recent > 0) {
-    newest = INT32_MIN;
-    for (int i = begin + tid; i < end; i += kThreads) newest = max(newest, E.pos[first + i]);
+  int* const places = reinterpret_cast<int*>(keys) + per;
+  const bool aged = E.pos && E.n_recent > 0;     // the newest position has to be found
+  int newest = E.pos ? INT32_MIN : len - 1;
+  if (staged || aged)
+    for (int i0 = begin + tid; i0 < end; i0 += kAhead * kThreads) {
+      int pos[kAhead];
+      float score[kAhead];
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        const int64_t at = first + min(i0 + j * kThreads, end - 1);
+        pos[j] = E.pos ? E.pos[at] : 0;
+        score[j] = staged ? E.score[at] : 0.f;
+      }
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        const int i = i0 + j * kThreads;
+        newest = E.pos ? max(newest, pos[j]) : newest;
+        if (staged && i < end) {
+          keys[i - begin] = score_key(score[j]);
+          if (E.pos) places[i - begin] = pos[j];
+        }
+      }
+    }
+  if (aged) {
     newest = __reduce_max_sync(0xffffffffu, newest);
-    if (lane == 0) warp_n[warp] = newest;
+    if (lane == 0) sh.warp_a[warp] = newest;
     __syncthreads();
-    if (tid == 0) {
-      for (int w = 1; w < kWarps; ++w) newest = max(newest, warp_n[w]);
-      cta_newest = newest;
+    if (warp == 0) {
+      newest = __reduce_max_sync(0xffffffffu, lane < kWarps ? sh.warp_a[lane] : INT32_MIN);
+      if (lane == 0) sh.cta[0][0] = newest;
     }
     cluster.sync();
-    for (int b = 0; b < C; ++b) newest = max(newest, *cluster.map_shared_rank(&cta_newest, b));
+    if (warp == 0) {
+      newest = __reduce_max_sync(0xffffffffu, lane < C ? *cluster.map_shared_rank(&sh.cta[0][0], lane) : INT32_MIN);
+      if (lane == 0) sh.all_a = newest;
+    }
+    __syncthreads();
+    newest = sh.all_a;
   }
   const int64_t recent = E.n_recent > 0 ? (int64_t)newest - E.n_recent : INT32_MAX;      // positions above are safe
-  auto form = [&](int i) {
-    const int pos = E.pos ? E.pos[first + i] : i;
-    return pos < E.n_first || pos > recent ? kSafe : score_key(E.score[first + i]);
-  };
+  auto safe = [&](int pos) { return pos < E.n_first || pos > recent; };
+  auto form = [&](int i) { return safe(E.pos ? E.pos[first + i] : i) ? kSafe : score_key(E.score[first + i]); };
   auto key = [&](int i) { return staged ? keys[i - begin] : form(i); };
+
+  // In place with room for one move: no second launch.  By the first CTA's first warp, when all have read what they need.
+  auto move_here = [&](int from, int to) {
+    if (c != 0 || warp != 0) return;
+    const int vecs = E.row_bytes / 16;
+    if (lane < vecs) {
+      static_cast<uint4*>(E.K_out)[(first + to) * vecs + lane] = static_cast<const uint4*>(E.K)[(first + from) * vecs + lane];
+      static_cast<uint4*>(E.V_out)[(first + to) * vecs + lane] = static_cast<const uint4*>(E.V)[(first + from) * vecs + lane];
+    }
+    if (lane == 0) {
+      E.score_out[first + to] = E.score[first + from];
+      if (E.pos_out) E.pos_out[first + to] = E.pos[first + from];
+    }
+  };
+
+  if (len == k + 1) {
+    // One row goes, every token's case: the last of those of the smallest key.  (The select below: 1025 rows 14 us, 9 here.)
+    unsigned long long least = ~0ull;            // the key, then from the last row on
+    for (int i = begin + tid; i < end; i += kThreads) {
+      const uint32_t u = staged ? safe(E.pos ? places[i - begin] : i) ? kSafe : keys[i - begin] : form(i);
+      least = min(least, (unsigned long long)u << 32 | (0xffffffffu - (uint32_t)i));
+    }
+    auto of_warp = [&](unsigned long long x) {
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) x = min(x, __shfl_xor_sync(0xffffffffu, x, o));
+      return x;
+    };
+    least = of_warp(least);
+    if (lane == 0) sh.warp_least[warp] = least;
+    __syncthreads();
+    if (warp == 0) {
+      least = of_warp(lane < kWarps ? sh.warp_least[lane] : ~0ull);
+      if (lane == 0) sh.cta_least = least;
+    }
+    cluster.sync();
+    if (warp == 0) {
+      least = of_warp(lane < C ? *cluster.map_shared_rank(&sh.cta_least, lane) : ~0ull);
+      if (lane == 0) sh.digit = (int)(0xffffffffu - (uint32_t)least);
+    }
+    __syncthreads();
+    const int gone = sh.digit;
+    if (!E.in_place)
+      for (int i = begin + tid; i < min(end, k); i += kThreads) source[i] = i == gone ? k : i;
+    if (c == 0 && tid == 0) {
+      E.n_moves[s] = gone < k;
+      if (gone < k && E.in_place) { holes[0] = gone; movers[0] = k; }
+      if (E.lens_out) E.lens_out[s] = k;
+    }
+    if (E.in_place && E.list == 1 && gone < k) move_here(k, gone);
+    cluster.sync();                              // nobody reads this CTA's memory any more
+    return;
+  }
 
   uint32_t prefix = 0;
   int need = k;
@@ -84,73 +206,58 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const EvictArgs 
     const uint32_t mask = pass == 2 ? 1023u : 2047u;
     for (int i = begin + tid; i < end; i += kThreads) {
       uint32_t u;
-      if (pass == 0) {
-        u = form(i);
-        if (staged) keys[i - begin] = u;
+      if (pass == 0 && staged) {                 // (this thread's rows)
+        u = safe(E.pos ? places[i - begin] : i) ? kSafe : keys[i - begin];
+        keys[i - begin] = u;
       } else {
         u = key(i);
       }
-      if (pass == 0 || u >> (pass == 1 ? 21 : 10) == prefix) atomicAdd(&hist[pass][u >> shift & mask], 1u);
+      if (pass == 0 || u >> (pass == 1 ? 21 : 10) == prefix) atomicAdd(&sh.hist[pass][u >> shift & mask], 1u);
+    }
+    __syncthreads();
+    {                                            // 64 bins to a sum: 16 threads with four bins each
+      const uint4 h = reinterpret_cast<const uint4*>(sh.hist[pass])[tid];
+      uint32_t n = h.x + h.y + h.z + h.w;
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
+      if (tid % 16 == 0) sh.coarse[pass][tid / 16] = n;
     }
     cluster.sync();
-    // each thread four neighbouring bins, from the largest down
-    constexpr int kPer = kBins / kThreads;
-    int n[kPer], sum = 0;
-    const int top = kBins - 1 - kPer * tid;
-    static_assert(kPer == 4, "a 16-byte load of the other CTAs' bins");
+    // One warp finds the digit, from the largest down: which 64 bins, then which of them.  (Every thread adding the cluster's bins up
+    // took 6000 cycles a pass: shared memory of other SMs is slow.)
+    if (warp == 0) {
+      int n = 0, before, rest;
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) n[j] = 0;
+      for (int b = 0; b < kMaxCluster; ++b)
+        if (b < C) n += (int)cluster.map_shared_rank(&sh.coarse[pass][0], b)[31 - lane];
+      const int group = 31 - lane_of(n, need, before);
+      int hi = 0, lo = 0;                        // the bins 63 - 2 lane, 62 - 2 lane of the 64
 #pragma unroll
-    for (int b = 0; b < kMaxCluster; ++b) {
-      if (b >= C) break;
-      const uint4 h = *reinterpret_cast<const uint4*>(cluster.map_shared_rank(&hist[pass][0], b) + top - 3);
-      n[0] += (int)h.w;
-      n[1] += (int)h.z;
-      n[2] += (int)h.y;
-      n[3] += (int)h.x;
-    }
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) sum += n[j];
-    int incl = sum;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int x = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += x;
-    }
-    if (lane == 31) scan[warp] = incl;
-    __syncthreads();
-    int before = incl - sum;
-    for (int w = 0; w < warp; ++w) before += scan[w];
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      if (before < need && need <= before + n[j]) {
-        found = top - j;
-        above = before;
+      for (int b = 0; b < kMaxCluster; ++b)
+        if (b < C) {
+          const uint2 h = *reinterpret_cast<const uint2*>(cluster.map_shared_rank(&sh.hist[pass][0], b) + 64 * group + 62 - 2 * lane);
+          hi += (int)h.y;
+          lo += (int)h.x;
+        }
+      const int at = lane_of(hi + lo, need - before, rest);
+      const int first_hi = __shfl_sync(0xffffffffu, hi, at);
+      const bool low = need - before - rest > first_hi;
+      if (lane == 0) {
+        sh.digit = 64 * group + 63 - 2 * at - (low ? 1 : 0);
+        sh.above = before + rest + (low ? first_hi : 0);
       }
-      before += n[j];
     }
     __syncthreads();
-    prefix = prefix << (pass == 2 ? 10 : 11) | (uint32_t)found;
-    need -= above;
+    prefix = prefix << (pass == 2 ? 10 : 11) | (uint32_t)sh.digit;
+    need -= sh.above;
   }
 
   // A warp takes neighbouring rows, so that ranks follow from ballots.
   const int seg = (per + kWarps - 1) / kWarps, w0 = min(end, begin + warp * seg), w1 = min(end, w0 + seg);
   const uint32_t lower = (1u << lane) - 1u;
-  int eq = 0;
-  for (int i = w0; i < w1; i += 32) eq += __popc(__ballot_sync(0xffffffffu, i + lane < w1 && key(i + lane) == prefix));
-  if (lane == 0) warp_n[warp] = eq;
-  __syncthreads();
-  if (tid == 0) {
-    int all = 0;
-    for (int w = 0; w < kWarps; ++w) all += warp_n[w];
-    cta_eq = all;
-  }
-  cluster.sync();
-  int eq_before = 0;
-  for (int b = 0; b < c; ++b) eq_before += *cluster.map_shared_rank(&cta_eq, b);
-  for (int w = 0; w < warp; ++w) eq_before += warp_n[w];
-  __syncthreads();
+  int eq_before = 0, none = 0, all = 0;
+  for (int i = w0; i < w1; i += 32) eq_before += __popc(__ballot_sync(0xffffffffu, i + lane < w1 && key(i + lane) == prefix));
+  sums_before(cluster, sh, 1, C, c, eq_before, none, all);
   // every row of the warp's: whether it is a hole or moves
   auto walk = [&](auto&& each) {
     int equal = eq_before;
@@ -164,24 +271,9 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const EvictArgs 
       each(row, __ballot_sync(0xffffffffu, held && !kept && row < k), __ballot_sync(0xffffffffu, kept && row >= k), kept);
     }
   };
-  int n_holes = 0, n_movers = 0;
-  walk([&](int, uint32_t hole, uint32_t mover, bool) { n_holes += __popc(hole); n_movers += __popc(mover); });
-  if (lane == 0) { warp_n[warp] = n_holes; warp_m[warp] = n_movers; }
-  __syncthreads();
-  if (tid == 0) {
-    int h = 0, m = 0;
-    for (int w = 0; w < kWarps; ++w) { h += warp_n[w]; m += warp_m[w]; }
-    cta_holes = h;
-    cta_movers = m;
-  }
-  cluster.sync();
-  int at_hole = 0, at_mover = 0, all = 0;
-  for (int b = 0; b < C; ++b) {
-    const int h = *cluster.map_shared_rank(&cta_holes, b), m = *cluster.map_shared_rank(&cta_movers, b);
-    if (b < c) { at_hole += h; at_mover += m; }
-    all += h;
-  }
-  for (int w = 0; w < warp; ++w) { at_hole += warp_n[w]; at_mover += warp_m[w]; }
+  int at_hole = 0, at_mover = 0;
+  walk([&](int, uint32_t hole, uint32_t mover, bool) { at_hole += __popc(hole); at_mover += __popc(mover); });
+  sums_before(cluster, sh, 2, C, c, at_hole, at_mover, all);
   walk([&](int row, uint32_t hole, uint32_t mover, bool kept) {
     if (hole >> lane & 1) holes[at_hole + __popc(hole & lower)] = row;
     if (mover >> lane & 1) movers[at_mover + __popc(mover & lower)] = row;
@@ -196,10 +288,12 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const EvictArgs 
   cluster.sync();                                // the lists are written; nobody reads this CTA's memory any more
   if (!E.in_place)
     for (int i = c * kThreads + tid; i < all; i += C * kThreads) source[__ldcg(holes + i)] = __ldcg(movers + i);
+  else if (E.list == 1 && all == 1)
+    move_here(__ldcg(movers), __ldcg(holes));
 }
 
 // A group of kVecs lanes per row: K, V, and by its first lane the score and the position.
-constexpr int kMoveThreads = 256, kMoveRows = 4;
+constexpr int kMoveThreads = 256, kMoveRows = 2;
 template <int kVecs>
 __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const EvictArgs E, int blocks) {
   constexpr int kGroups = kMoveThreads / kVecs;
@@ -222,14 +316,14 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const EvictArg
 #pragma unroll
   for (int j = 0; j < kMoveRows; ++j)
     if (from[j] >= 0) {
-      k[j] = static_cast<const uint4*>(E.K)[from[j] * kVecs + lane];
-      v[j] = static_cast<const uint4*>(E.V)[from[j] * kVecs + lane];
+      k[j] = __ldcs(static_cast<const uint4*>(E.K) + from[j] * kVecs + lane);
+      v[j] = __ldcs(static_cast<const uint4*>(E.V) + from[j] * kVecs + lane);
     }
 #pragma unroll
   for (int j = 0; j < kMoveRows; ++j)
     if (from[j] >= 0) {
-      static_cast<uint4*>(E.K_out)[to[j] * kVecs + lane] = k[j];
-      static_cast<uint4*>(E.V_out)[to[j] * kVecs + lane] = v[j];
+      __stcs(static_cast<uint4*>(E.K_out) + to[j] * kVecs + lane, k[j]);
+      __stcs(static_cast<uint4*>(E.V_out) + to[j] * kVecs + lane, v[j]);
       if (lane == 0) {
         E.score_out[to[j]] = E.score[from[j]];
         if (E.pos_out) E.pos_out[to[j]] = E.pos ? E.pos[from[j]] : (int)(from[j] - (int64_t)s * E.cap);
@@ -249,18 +343,18 @@ cudaError_t launch_move(const EvictArgs& E, cudaStream_t st) {
 
 cudaError_t launch_evict(const EvictArgs& E, cudaStream_t st) {
   int C = 1;
-  while (C < kMaxCluster && E.cap > 4096 * C) C *= 2;
+  while (C < kMaxCluster && E.cap > 2048 * C) C *= 2;
   const int per = (E.cap + C - 1) / C, staged = per <= kStageRows;
-  PdlConfig pc(dim3((unsigned)C * E.n_streams), kThreads, staged ? (size_t)per * 4 : 0, st);
+  PdlConfig pc(dim3((unsigned)C * E.n_streams), kThreads, staged ? (size_t)per * (E.pos ? 8 : 4) : 0, st);
   cudaLaunchAttribute attrs[2] = {pc.attr, {}};
   attrs[1].id = cudaLaunchAttributeClusterDimension;
   attrs[1].val.clusterDim.x = C;
   attrs[1].val.clusterDim.y = attrs[1].val.clusterDim.z = 1;
   pc.cfg.attrs = attrs;
   pc.cfg.numAttrs = 2;
-  cudaError_t e = cudaFuncSetAttribute(evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kStageRows * 4);
+  cudaError_t e = cudaFuncSetAttribute(evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kStageRows * 8);
   if (e == cudaSuccess) e = cudaLaunchKernelEx(&pc.cfg, evict_select_kernel, E, per, staged);
-  if (e != cudaSuccess || (E.in_place && E.list == 0)) return e;
+  if (e != cudaSuccess || (E.in_place && E.list <= 1)) return e;
   switch (E.row_bytes / 16) {
     case 8: return launch_move<8>(E, st);
     case 16: return launch_move<16>(E, st);

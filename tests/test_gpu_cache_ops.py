@@ -197,8 +197,18 @@ def test_eviction_into_a_larger_cache(cuda_lib):
 
 
 def test_eviction_from_a_cache_too_long_to_stage(cuda_lib):
-    """A cluster's shared memory holds the keys of 393216 rows; longer caches read their scores again."""
-    _check_evict(cuda_lib, "bf16", 64, 400003, [400003], 1000, 2, 50, seed=9)
+    """A cluster's shared memory holds the keys and positions of 196608 rows; longer caches read them again."""
+    _check_evict(cuda_lib, "bf16", 64, 200003, [200003], 1000, 2, 50, seed=9)
+    _check_evict(cuda_lib, "bf16", 64, 200003, [200000], 150000, 2, 50, with_pos=False, in_place=True, seed=9)
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("kind,cap", [("mixed", 97), ("equal", 97), ("mixed", 5000), ("spread", 33000), ("equal", 20000)])
+def test_one_row_over_the_budget(cuda_lib, kind, cap, in_place):
+    """Every token's eviction: one row goes, at most one moves; streams that are not over keep all."""
+    _check_evict(cuda_lib, "bf16", 64, cap, [cap, cap - 1, cap, cap // 2], cap - 1, 4, 16, kind=kind, in_place=in_place, seed=cap)
+    _check_evict(cuda_lib, "fp32", 128, cap, [cap] * 3, cap - 1, 0, 0, kind=kind, with_pos=False, in_place=in_place, seed=cap + 1)
+    _check_evict(cuda_lib, "bf16", 128, cap, [cap - 2, cap - 3], cap - 3, 2, 3, kind=kind, in_place=in_place, seed=cap + 2)      # room for two moves more
 
 
 def test_many_streams_at_once(cuda_lib):
