@@ -455,26 +455,42 @@ def decode_attn_static_status(stream=None):
     return v.value
 
 
-def _expect(what, device, name, t, dtype, shape):
-    """``t`` (or None) is a contiguous tensor of this dtype and shape on CUDA device number ``device``."""
-    if t is None or (t.dtype is dtype and t.shape == shape and t.get_device() == device and t.is_contiguous()):
-        return
-    if t.dtype is not dtype or t.shape != shape:
-        raise ValueError(f"{what}: {name}: expected dtype {dtype} and shape {tuple(shape)}, got {t.dtype} and {tuple(t.shape)}")
-    raise ValueError(f"{what}: {name}: expected a contiguous tensor on CUDA device {device}")
+def _is(t, dtype, shape, device):
+    """A contiguous tensor of this dtype and shape on CUDA device number ``device``, or None."""
+    return t is None or (t.dtype is dtype and t.shape == shape and t.get_device() == device and t.is_contiguous())
+
+
+def _expect(what, device, **tensors):
+    """Says which of the tensors (each with its dtype and shape) is not what it should be."""
+    for name, (t, dtype, shape) in tensors.items():
+        if t is None:
+            continue
+        if t.dtype is not dtype or t.shape != shape:
+            raise ValueError(f"{what}: {name}: expected dtype {dtype} and shape {tuple(shape)}, got {t.dtype} and {tuple(t.shape)}")
+        if t.get_device() != device or not t.is_contiguous():
+            raise ValueError(f"{what}: {name}: expected a contiguous tensor on the device of the first")
 
 
 def _on_current(what, device, t):
     """The call runs on a stream of the current CUDA device, which has to be the tensors'."""
-    import torch
-
-    if device < 0 or device != torch._C._cuda_getDevice():
+    if device < 0 or device != _torch()._C._cuda_getDevice():
         raise ValueError(f"{what}: the tensors are on {t.device}, not on the current CUDA device")
 
 
-def _dtype_code(what, dtype):
-    import torch
+def _torch():
+    global _torch_module
+    if _torch_module is None:
+        import torch
 
+        _torch_module = torch
+    return _torch_module
+
+
+_torch_module = None
+
+
+def _dtype_code(what, dtype):
+    torch = _torch()
     if dtype is torch.bfloat16:
         return 1
     if dtype is torch.float32:
@@ -488,8 +504,7 @@ def _ptr(t):
 
 def _on_stream(stream):
     """Tensors made inside belong to the stream of the call, so that their memory is not handed on while it still runs."""
-    import torch
-
+    torch = _torch()
     if isinstance(stream, int):
         stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
     return torch.cuda.stream(stream)
@@ -504,8 +519,7 @@ def _workspace_bytes(name, *sizes):
 
 
 def _workspace(device, size):
-    import torch
-
+    torch = _torch()
     return torch.empty(size, dtype=torch.uint8, device=device) if size else None
 
 
@@ -516,25 +530,22 @@ def attn_scored(K, V, q, lens=None, score=None, score_out=None, n_scored=None, d
     lens: int32 [n_streams], rows in use (None: all).  The newest ``n_scored`` queries (None: all) add their weights to ``decay`` times
     ``score`` (float32 [n_streams, capacity]; None: zeros); the result goes to ``score_out``, by default ``score`` itself or a
     new tensor of zeros.  Returns (out, score_out); with n_scored = 0 the second is ``score_out`` as it was."""
-    import torch
-
     if stream is not None:
         with _on_stream(stream):
             return attn_scored(K, V, q, lens, score, score_out, n_scored, decay, out)
-    what = "balancekv_attn_scored"
-    if K.dim() != 3 or q.dim() not in (3, 4):
+    what, torch = "balancekv_attn_scored", _torch()
+    ks, qs = K.shape, q.shape
+    if len(ks) != 3 or len(qs) not in (3, 4):
         raise ValueError(f"{what}: expected K [n_streams, capacity, d] and q [n_streams, group, (n_queries,) d]")
-    (S, cap, d), group, m = K.shape, q.shape[1], q.shape[2] if q.dim() == 4 else 1
-    dtype, code, device = K.dtype, _dtype_code(what, K.dtype), K.get_device()
+    (S, cap, d), group, m = ks, qs[1], qs[2] if len(qs) == 4 else 1
+    dtype, device, ss, f32 = K.dtype, K.get_device(), (S, cap), torch.float32
+    code = _dtype_code(what, dtype)
     if n_scored is None:
         n_scored = m
-    _expect(what, device, "K", K, dtype, (S, cap, d))
-    _expect(what, device, "V", V, dtype, (S, cap, d))
-    _expect(what, device, "q", q, dtype, (S, group, m, d) if q.dim() == 4 else (S, group, d))
-    _expect(what, device, "out", out, dtype, q.shape)
-    _expect(what, device, "lens", lens, torch.int32, (S,))
-    _expect(what, device, "score", score, torch.float32, (S, cap))
-    _expect(what, device, "score_out", score_out, torch.float32, (S, cap))
+    if not (qs[0] == S and qs[-1] == d and _is(K, dtype, ks, device) and _is(V, dtype, ks, device) and _is(q, dtype, qs, device) and _is(out, dtype, qs, device)
+            and _is(lens, torch.int32, (S,), device) and _is(score, f32, ss, device) and _is(score_out, f32, ss, device)):
+        _expect(what, device, K=(K, dtype, ks), V=(V, dtype, ks), q=(q, dtype, (S, *qs[1:-1], d)), out=(out, dtype, qs), lens=(lens, torch.int32, (S,)),
+                score=(score, f32, ss), score_out=(score_out, f32, ss))
     _on_current(what, device, K)
     if out is None:
         out = torch.empty_like(q)
@@ -554,26 +565,24 @@ def cache_evict(K, V, score, n_keep, lens=None, pos=None, n_first=0, n_recent=0,
     lens: int32 [n_streams] (None: all rows are in use).  ``out``: a dict of "k", "v", "score" and, if they are wanted, "pos" and "lens" to
     fill, by default new tensors of min(n_keep, capacity) rows whose unused ones are zero; with ``in_place`` the cache itself, of which only
     the rows that fill a hole move (``pos`` and ``lens`` are updated if given, ``lens`` is made if not).  Returns that dict."""
-    import torch
-
     if stream is not None:
         with _on_stream(stream):
             return cache_evict(K, V, score, n_keep, lens, pos, n_first, n_recent, out, in_place)
-    what = "balancekv_cache_evict"
-    if K.dim() != 3:
+    what, torch = "balancekv_cache_evict", _torch()
+    ks = K.shape
+    if len(ks) != 3:
         raise ValueError(f"{what}: expected K [n_streams, capacity, d]")
-    S, cap, d = K.shape
-    dtype, code, device = K.dtype, _dtype_code(what, K.dtype), K.get_device()
-    _expect(what, device, "K", K, dtype, (S, cap, d))
-    _expect(what, device, "V", V, dtype, (S, cap, d))
-    _expect(what, device, "score", score, torch.float32, (S, cap))
-    _expect(what, device, "pos", pos, torch.int32, (S, cap))
-    _expect(what, device, "lens", lens, torch.int32, (S,))
+    S, cap, d = ks
+    dtype, device, ss, i32, f32 = K.dtype, K.get_device(), (S, cap), torch.int32, torch.float32
+    code = _dtype_code(what, dtype)
+    if not (score is not None and _is(K, dtype, ks, device) and _is(V, dtype, ks, device) and _is(score, f32, ss, device) and _is(pos, i32, ss, device)
+            and _is(lens, i32, (S,), device)):
+        _expect(what, device, K=(K, dtype, ks), V=(V, dtype, ks), score=(score, f32, ss), pos=(pos, i32, ss), lens=(lens, i32, (S,)))
     _on_current(what, device, K)
     if in_place:
         if out is not None:
             raise ValueError(f"{what}: either out or in_place")
-        out = {"k": K, "v": V, "score": score, "pos": pos, "lens": torch.empty(S, dtype=torch.int32, device=K.device) if lens is None else lens}
+        out = {"k": K, "v": V, "score": score, "pos": pos, "lens": torch.empty(S, dtype=i32, device=K.device) if lens is None else lens}
         Ko, Vo, so, po, lo, rows = K, V, score, pos, out["lens"], cap
     else:
         if out is None:
@@ -581,19 +590,19 @@ def cache_evict(K, V, score, n_keep, lens=None, pos=None, n_first=0, n_recent=0,
             if rows < 1:
                 raise ValueError(f"{what}: n_keep and the capacity are at least 1")
             out = {"k": K.new_zeros(S, rows, d), "v": V.new_zeros(S, rows, d), "score": score.new_zeros(S, rows),
-                   "pos": torch.zeros(S, rows, dtype=torch.int32, device=K.device), "lens": torch.empty(S, dtype=torch.int32, device=K.device)}
+                   "pos": torch.zeros(S, rows, dtype=i32, device=K.device), "lens": torch.empty(S, dtype=i32, device=K.device)}
         Ko, Vo, so, po, lo = out["k"], out["v"], out["score"], out.get("pos"), out.get("lens")
         rows = Ko.shape[1] if Ko.dim() == 3 else 0
-        _expect(what, device, "out k", Ko, dtype, (S, rows, d))
-        _expect(what, device, "out v", Vo, dtype, (S, rows, d))
-        _expect(what, device, "out score", so, torch.float32, (S, rows))
-        _expect(what, device, "out pos", po, torch.int32, (S, rows))
-        _expect(what, device, "out lens", lo, torch.int32, (S,))
-    size = _workspace_bytes(what, S, cap, n_keep, d, code, int(Ko.data_ptr() == K.data_ptr()))
+        os = (S, rows)
+        if not (_is(Ko, dtype, (S, rows, d), device) and _is(Vo, dtype, (S, rows, d), device) and _is(so, f32, os, device) and _is(po, i32, os, device)
+                and _is(lo, i32, (S,), device)):
+            _expect(what, device, out_k=(Ko, dtype, (S, rows, d)), out_v=(Vo, dtype, (S, rows, d)), out_score=(so, f32, os), out_pos=(po, i32, os),
+                    out_lens=(lo, i32, (S,)))
+    k, ko = K.data_ptr(), Ko.data_ptr()
+    size = _workspace_bytes(what, S, cap, n_keep, d, code, int(ko == k))
     ws = _workspace(K.device, size)
-    _check(load().balancekv_cache_evict(K.data_ptr(), V.data_ptr(), score.data_ptr(), _ptr(pos), _ptr(lens), S, cap, Ko.data_ptr(), Vo.data_ptr(),
-                                        so.data_ptr(), _ptr(po), _ptr(lo), rows, n_keep, n_first, n_recent, d, code, _ptr(ws), size,
-                                        _stream_ptr(None)), what)
+    _check(load().balancekv_cache_evict(k, V.data_ptr(), _ptr(score), _ptr(pos), _ptr(lens), S, cap, ko, Vo.data_ptr(), _ptr(so), _ptr(po), _ptr(lo), rows,
+                                        n_keep, n_first, n_recent, d, code, _ptr(ws), size, _stream_ptr(None)), what)
     return out
 
 
@@ -603,26 +612,22 @@ def decode_attn_prefix(K_prefix, V_prefix, K, V, q, lens=None, weight=None, out=
     K_prefix, V_prefix: CUDA tensors [n_kv_heads, prefix_len, d]; weight: float32 [n_kv_heads, prefix_len] (None: ones);
     K, V: [n_seqs, n_kv_heads, capacity, d], or None where the sequences have no rows of their own; lens: int32 [n_seqs] (None: all rows
     are in use); q: [n_seqs, n_kv_heads * group, d]."""
-    import torch
-
     if stream is not None:
         with _on_stream(stream):
             return decode_attn_prefix(K_prefix, V_prefix, K, V, q, lens, weight, out)
-    what = "balancekv_decode_attn_prefix"
-    if K_prefix.dim() != 3 or q.dim() != 3 or (K is None) != (V is None) or (K is not None and K.dim() != 4):
+    what, torch = "balancekv_decode_attn_prefix", _torch()
+    ps, qs = K_prefix.shape, q.shape
+    if len(ps) != 3 or len(qs) != 3 or (K is None) != (V is None) or (K is not None and K.dim() != 4):
         raise ValueError(f"{what}: expected K_prefix [n_kv_heads, prefix_len, d], K [n_seqs, n_kv_heads, capacity, d] and q [n_seqs, n_q_heads, d]")
-    (H, P, d), (B, Hq, _), cap = K_prefix.shape, q.shape, 0 if K is None else K.shape[2]
+    (H, P, d), (B, Hq, _), cap = ps, qs, 0 if K is None else K.shape[2]
     if H < 1 or Hq % H:
         raise ValueError(f"{what}: {Hq} query heads do not share {H} KV heads")
-    dtype, code, device = K_prefix.dtype, _dtype_code(what, K_prefix.dtype), K_prefix.get_device()
-    _expect(what, device, "K_prefix", K_prefix, dtype, (H, P, d))
-    _expect(what, device, "V_prefix", V_prefix, dtype, (H, P, d))
-    _expect(what, device, "K", K, dtype, (B, H, cap, d))
-    _expect(what, device, "V", V, dtype, (B, H, cap, d))
-    _expect(what, device, "q", q, dtype, (B, Hq, d))
-    _expect(what, device, "out", out, dtype, (B, Hq, d))
-    _expect(what, device, "weight", weight, torch.float32, (H, P))
-    _expect(what, device, "lens", lens, torch.int32, (B,))
+    dtype, device, ks, f32 = K_prefix.dtype, K_prefix.get_device(), (B, H, cap, d), torch.float32
+    code = _dtype_code(what, dtype)
+    if not (qs[2] == d and _is(K_prefix, dtype, ps, device) and _is(V_prefix, dtype, ps, device) and _is(K, dtype, ks, device) and _is(V, dtype, ks, device)
+            and _is(q, dtype, qs, device) and _is(out, dtype, qs, device) and _is(weight, f32, (H, P), device) and _is(lens, torch.int32, (B,), device)):
+        _expect(what, device, K_prefix=(K_prefix, dtype, ps), V_prefix=(V_prefix, dtype, ps), K=(K, dtype, ks), V=(V, dtype, ks), q=(q, dtype, (B, Hq, d)),
+                out=(out, dtype, qs), weight=(weight, f32, (H, P)), lens=(lens, torch.int32, (B,)))
     _on_current(what, device, K_prefix)
     if out is None:
         out = torch.empty_like(q)

@@ -695,7 +695,8 @@ cudaError_t launch_few(const FewArgs& P, const FewArgs* also, cudaStream_t st) {
   if (ctas > INT32_MAX) return cudaErrorInvalidValue;
   return for_rows<kBf16, D>(most, [&](auto rows) {
     auto kern = attn_few_kernel<kBf16, D, decltype(rows)::value>;
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)F::kSmem);
+    static std::atomic<unsigned long long> devices{0};
+    const cudaError_t e = kernel_limits(kern, F::kSmem, false, devices);
     if (e != cudaSuccess) return e;
     const PdlConfig pc(dim3((unsigned)ctas), kThreads, F::kSmem, st);
     return cudaLaunchKernelEx(&pc.cfg, kern, J, maps);
@@ -714,8 +715,8 @@ cudaError_t launch_cluster(const AttnRows& A, const ScoreArgs& S, int C, float* 
   const int groups = (A.n_rows + kFewRows - 1) / kFewRows;
   e = for_rows<kBf16, D>(A.n_rows, [&](auto rows) {
     auto kern = attn_few_cluster_kernel<kBf16, D, decltype(rows)::value>;
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)F::kSmem + logit_bytes(kBf16, D));
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    static std::atomic<unsigned long long> devices{0};
+    const cudaError_t e = kernel_limits(kern, F::kSmem + logit_bytes(kBf16, D), true, devices);
     if (e != cudaSuccess) return e;
     const int pitch = logit_pitch(A.cap, C);
     PdlConfig pc(dim3(A.n_streams * groups, C), kThreads, F::kSmem + (size_t)std::min(A.n_rows, kFewRows) * pitch * 4, st);

@@ -233,13 +233,26 @@ __global__ void __launch_bounds__(kThreads) score_simt_kernel(const AttnRows A, 
 }
 
 template <class Kern, class... Args>
-cudaError_t launch(Kern kern, dim3 grid, size_t smem, cudaStream_t st, const Args&... args) {
-  if (smem) {
-    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return e;
-  }
+cudaError_t launch(Kern kern, std::atomic<unsigned long long>& devices, dim3 grid, size_t smem, cudaStream_t st, const Args&... args) {
+  const cudaError_t e = kernel_limits(kern, smem, false, devices);
+  if (e != cudaSuccess) return e;
   const PdlConfig pc(grid, kThreads, smem, st);
   return cudaLaunchKernelEx(&pc.cfg, kern, args...);
+}
+template <bool kBf16, int D>
+cudaError_t attn(const AttnRows& A, dim3 grid, int tiles, cudaStream_t st) {
+  static std::atomic<unsigned long long> devices{0};
+  return launch(attn_simt_kernel<kBf16, D>, devices, grid, Tile<D>::kSmem, st, A, tiles);
+}
+template <bool kBf16, int D>
+cudaError_t score(const AttnRows& A, const ScoreArgs& S, dim3 grid, int tiles, cudaStream_t st) {
+  static std::atomic<unsigned long long> devices{0};
+  return launch(score_simt_kernel<kBf16, D>, devices, grid, Tile<D>::kSmem, st, A, S, tiles);
+}
+template <bool kBf16, int D>
+cudaError_t combine(const AttnRows& A, cudaStream_t st) {
+  const PdlConfig pc(dim3(join_ctas(A)), kThreads, 0, st);
+  return cudaLaunchKernelEx(&pc.cfg, attn_combine_kernel<kBf16, D>, A);
 }
 
 }  // namespace
@@ -247,21 +260,20 @@ cudaError_t launch(Kern kern, dim3 grid, size_t smem, cudaStream_t st, const Arg
 cudaError_t launch_attn_simt(const AttnRows& A, int d, int is_bf16, cudaStream_t st) {
   const int tiles = (A.n_rows + kRows - 1) / kRows;
   const dim3 grid((unsigned)tiles * A.n_streams, A.splits);
-  if (d == 128) return is_bf16 ? launch(attn_simt_kernel<true, 128>, grid, Tile<128>::kSmem, st, A, tiles) : launch(attn_simt_kernel<false, 128>, grid, Tile<128>::kSmem, st, A, tiles);
-  return is_bf16 ? launch(attn_simt_kernel<true, 64>, grid, Tile<64>::kSmem, st, A, tiles) : launch(attn_simt_kernel<false, 64>, grid, Tile<64>::kSmem, st, A, tiles);
+  if (d == 128) return is_bf16 ? attn<true, 128>(A, grid, tiles, st) : attn<false, 128>(A, grid, tiles, st);
+  return is_bf16 ? attn<true, 64>(A, grid, tiles, st) : attn<false, 64>(A, grid, tiles, st);
 }
 
 cudaError_t launch_attn_combine(const AttnRows& A, int d, int is_bf16, cudaStream_t st) {
-  const dim3 grid(join_ctas(A));
-  if (d == 128) return is_bf16 ? launch(attn_combine_kernel<true, 128>, grid, 0, st, A) : launch(attn_combine_kernel<false, 128>, grid, 0, st, A);
-  return is_bf16 ? launch(attn_combine_kernel<true, 64>, grid, 0, st, A) : launch(attn_combine_kernel<false, 64>, grid, 0, st, A);
+  if (d == 128) return is_bf16 ? combine<true, 128>(A, st) : combine<false, 128>(A, st);
+  return is_bf16 ? combine<true, 64>(A, st) : combine<false, 64>(A, st);
 }
 
 cudaError_t launch_score_simt(const AttnRows& A, const ScoreArgs& S, int d, int is_bf16, cudaStream_t st) {
   const int tiles = (A.cap + kKeys - 1) / kKeys;
   const dim3 grid((unsigned)tiles * A.n_streams);
-  if (d == 128) return is_bf16 ? launch(score_simt_kernel<true, 128>, grid, Tile<128>::kSmem, st, A, S, tiles) : launch(score_simt_kernel<false, 128>, grid, Tile<128>::kSmem, st, A, S, tiles);
-  return is_bf16 ? launch(score_simt_kernel<true, 64>, grid, Tile<64>::kSmem, st, A, S, tiles) : launch(score_simt_kernel<false, 64>, grid, Tile<64>::kSmem, st, A, S, tiles);
+  if (d == 128) return is_bf16 ? score<true, 128>(A, S, grid, tiles, st) : score<false, 128>(A, S, grid, tiles, st);
+  return is_bf16 ? score<true, 64>(A, S, grid, tiles, st) : score<false, 64>(A, S, grid, tiles, st);
 }
 
 }  // namespace bkv

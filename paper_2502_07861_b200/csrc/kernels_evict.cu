@@ -7,6 +7,8 @@
 // of a copy is another's destination.
 #include <cooperative_groups.h>
 
+#include <algorithm>
+
 #include "attn_rows.cuh"
 
 namespace bkv {
@@ -78,6 +80,40 @@ __device__ inline int lane_of(int n, int need, int& before) {
   return at;
 }
 
+// `rows` of a stream, the i-th from row from(i) to row to(i), by the threads that count from `at` in steps of `step`: K, V, score, position.
+template <class From, class To>
+__device__ inline void copy_rows(const EvictArgs& E, int s, int rows, int at, int step, From from, To to) {
+  constexpr int kBatch = 4;                      // rows in flight per thread
+  const int vecs = E.row_bytes / 16, lane = at % vecs, groups = step / vecs;
+  for (int i0 = at / vecs; i0 < rows; i0 += kBatch * groups) {
+    int64_t src[kBatch], dst[kBatch];
+    uint4 k[kBatch], v[kBatch];
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      const int i = min(i0 + j * groups, rows - 1);
+      src[j] = (int64_t)s * E.cap + from(i);
+      dst[j] = i0 + j * groups < rows ? (int64_t)s * E.cap_out + to(i) : -1;
+    }
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      k[j] = __ldcs(static_cast<const uint4*>(E.K) + src[j] * vecs + lane);
+      v[j] = __ldcs(static_cast<const uint4*>(E.V) + src[j] * vecs + lane);
+    }
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j)
+      if (dst[j] >= 0) {
+        __stcs(static_cast<uint4*>(E.K_out) + dst[j] * vecs + lane, k[j]);
+        __stcs(static_cast<uint4*>(E.V_out) + dst[j] * vecs + lane, v[j]);
+        if (lane == 0) {
+          E.score_out[dst[j]] = E.score[src[j]];
+          if (E.pos_out) E.pos_out[dst[j]] = E.pos ? E.pos[src[j]] : (int)(src[j] - (int64_t)s * E.cap);
+        }
+      }
+  }
+}
+
+// kFused: the clusters copy their streams' rows themselves.
+template <bool kFused>
 __global__ void __launch_bounds__(kThreads) evict_select_kernel(const EvictArgs E, int per, int staged) {
   extern __shared__ uint32_t keys[];             // [per], behind them the positions (E.pos) [per]
   __shared__ SelectShared sh;
@@ -93,7 +129,9 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const EvictArgs 
   int* source = movers + E.list;
   if (len <= E.keep) {                           // nothing to evict (the same for the whole cluster, which has read lens by its barrier)
     cluster.sync();
-    if (!E.in_place)
+    auto same = [](int i) { return i; };
+    if (kFused && !E.in_place) copy_rows(E, s, len, c * kThreads + tid, C * kThreads, same, same);
+    if (!kFused && !E.in_place)
       for (int i = c * kThreads + tid; i < len; i += C * kThreads) source[i] = i;
     if (c == 0 && tid == 0) {
       E.n_moves[s] = 0;
@@ -146,20 +184,6 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const EvictArgs 
   auto form = [&](int i) { return safe(E.pos ? E.pos[first + i] : i) ? kSafe : score_key(E.score[first + i]); };
   auto key = [&](int i) { return staged ? keys[i - begin] : form(i); };
 
-  // In place with room for one move: no second launch.  By the first CTA's first warp, when all have read what they need.
-  auto move_here = [&](int from, int to) {
-    if (c != 0 || warp != 0) return;
-    const int vecs = E.row_bytes / 16;
-    if (lane < vecs) {
-      static_cast<uint4*>(E.K_out)[(first + to) * vecs + lane] = static_cast<const uint4*>(E.K)[(first + from) * vecs + lane];
-      static_cast<uint4*>(E.V_out)[(first + to) * vecs + lane] = static_cast<const uint4*>(E.V)[(first + from) * vecs + lane];
-    }
-    if (lane == 0) {
-      E.score_out[first + to] = E.score[first + from];
-      if (E.pos_out) E.pos_out[first + to] = E.pos[first + from];
-    }
-  };
-
   if (len == k + 1) {
     // One row goes, every token's case: the last of those of the smallest key.  (The select below: 1025 rows 14 us, 9 here.)
     unsigned long long least = ~0ull;            // the key, then from the last row on
@@ -186,15 +210,24 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const EvictArgs 
     }
     __syncthreads();
     const int gone = sh.digit;
-    if (!E.in_place)
-      for (int i = begin + tid; i < min(end, k); i += kThreads) source[i] = i == gone ? k : i;
+    cluster.sync();                              // nobody reads this CTA's memory any more, nor what is copied over
     if (c == 0 && tid == 0) {
       E.n_moves[s] = gone < k;
-      if (gone < k && E.in_place) { holes[0] = gone; movers[0] = k; }
       if (E.lens_out) E.lens_out[s] = k;
     }
-    if (E.in_place && E.list == 1 && gone < k) move_here(k, gone);
-    cluster.sync();                              // nobody reads this CTA's memory any more
+    if (!E.in_place) {
+      auto from = [&](int i) { return i == gone ? k : i; };
+      if (kFused) copy_rows(E, s, k, c * kThreads + tid, C * kThreads, from, [](int i) { return i; });
+      else
+        for (int i = c * kThreads + tid; i < k; i += C * kThreads) source[i] = from(i);
+    } else if (gone < k) {
+      if (kFused) {
+        if (c == 0) copy_rows(E, s, 1, tid, kThreads, [&](int) { return k; }, [&](int) { return gone; });
+      } else if (c == 0 && tid == 0) {
+        holes[0] = gone;
+        movers[0] = k;
+      }
+    }
     return;
   }
 
@@ -288,8 +321,13 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const EvictArgs 
   cluster.sync();                                // the lists are written; nobody reads this CTA's memory any more
   if (!E.in_place)
     for (int i = c * kThreads + tid; i < all; i += C * kThreads) source[__ldcg(holes + i)] = __ldcg(movers + i);
-  else if (E.list == 1 && all == 1)
-    move_here(__ldcg(movers), __ldcg(holes));
+  if (!kFused) return;
+  if (E.in_place) {
+    copy_rows(E, s, all, c * kThreads + tid, C * kThreads, [&](int i) { return __ldcg(movers + i); }, [&](int i) { return __ldcg(holes + i); });
+    return;
+  }
+  cluster.sync();                                // the list of sources is whole
+  copy_rows(E, s, k, c * kThreads + tid, C * kThreads, [&](int i) { return __ldcg(source + i); }, [](int i) { return i; });
 }
 
 // A group of kVecs lanes per row: K, V, and by its first lane the score and the position.
@@ -344,6 +382,14 @@ cudaError_t launch_move(const EvictArgs& E, cudaStream_t st) {
 cudaError_t launch_evict(const EvictArgs& E, cudaStream_t st) {
   int C = 1;
   while (C < kMaxCluster && E.cap > 2048 * C) C *= 2;
+  // One launch where every CTA has an SM to itself and little to copy; larger clusters share the copying.  The second launch costs the
+  // host 2.5 us and the device 4; a CTA moves about 100 KB a microsecond, half of that where sources come from a list (1 stream, 4000 of 16000
+  // rows by 8 CTAs with 512 KB each: 26 us against 17 by two launches; 64 streams, 1024 of 1025: 15.6 us a call against 18.2).
+  const int64_t bytes = 4 * (int64_t)E.row_bytes * (E.in_place ? E.list : std::min(E.keep, E.cap));
+  int F = C;
+  while (F < kMaxCluster && 2 * F * E.n_streams <= kAttnSms && bytes > F * ((int64_t)128 << 10)) F *= 2;
+  const bool fused = (int64_t)F * E.n_streams <= kAttnSms && bytes <= F * ((int64_t)(E.cap - E.keep <= 1 ? 512 : 128) << 10);
+  if (fused) C = F;
   const int per = (E.cap + C - 1) / C, staged = per <= kStageRows;
   PdlConfig pc(dim3((unsigned)C * E.n_streams), kThreads, staged ? (size_t)per * (E.pos ? 8 : 4) : 0, st);
   cudaLaunchAttribute attrs[2] = {pc.attr, {}};
@@ -352,9 +398,11 @@ cudaError_t launch_evict(const EvictArgs& E, cudaStream_t st) {
   attrs[1].val.clusterDim.y = attrs[1].val.clusterDim.z = 1;
   pc.cfg.attrs = attrs;
   pc.cfg.numAttrs = 2;
-  cudaError_t e = cudaFuncSetAttribute(evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kStageRows * 8);
-  if (e == cudaSuccess) e = cudaLaunchKernelEx(&pc.cfg, evict_select_kernel, E, per, staged);
-  if (e != cudaSuccess || (E.in_place && E.list <= 1)) return e;
+  static std::atomic<unsigned long long> devices[2];
+  auto kern = fused ? evict_select_kernel<true> : evict_select_kernel<false>;
+  cudaError_t e = kernel_limits(kern, kStageRows * 8, false, devices[fused]);
+  if (e == cudaSuccess) e = cudaLaunchKernelEx(&pc.cfg, kern, E, per, staged);
+  if (e != cudaSuccess || fused || (E.in_place && E.list == 0)) return e;
   switch (E.row_bytes / 16) {
     case 8: return launch_move<8>(E, st);
     case 16: return launch_move<16>(E, st);

@@ -206,7 +206,8 @@ cudaError_t launch(const AttnRows& A, const ScoreArgs& S, cudaStream_t st) {
   CUtensorMap mq, mk;
   cudaError_t e = cache_map(&mq, A.q, true, D, A.n_queries, A.total_rows / A.n_queries, kTcRows);
   if (e == cudaSuccess) e = cache_map(&mk, A.K, true, D, A.cap, A.n_streams, kTcKeys);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(score_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Shape<D>::kSmem);
+  static std::atomic<unsigned long long> devices{0};
+  if (e == cudaSuccess) e = kernel_limits(score_tc_kernel<D>, Shape<D>::kSmem, false, devices);
   if (e != cudaSuccess) return e;
   const int blocks = (A.cap + 2 * kTcKeys - 1) / (2 * kTcKeys);
   const PdlConfig pc(dim3((unsigned)blocks * A.n_streams), kThreads, Shape<D>::kSmem, st);
