@@ -159,7 +159,7 @@ cudaError_t launch_score_simt(const AttnRows& A, const ScoreArgs& S, int d, int 
 
 int few_splits(int64_t streams, int cap, int n_rows);
 int64_t few_pitch(int cap);
-cudaError_t launch_attn_few(const AttnRows& A, float* x, const AttnRows* also, int d, int is_bf16, cudaStream_t st);
+cudaError_t launch_attn_few(const AttnRows& A, float* x, const AttnRows* also, bool finish, int d, int is_bf16, cudaStream_t st);
 int few_cluster(int64_t streams, int cap, int n_rows, int d, int is_bf16);
 int64_t few_cluster_sums(const AttnRows& A);
 cudaError_t launch_attn_few_cluster(const AttnRows& A, const ScoreArgs& S, int C, float* sums, int d, int is_bf16, cudaStream_t st);

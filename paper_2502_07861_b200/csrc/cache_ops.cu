@@ -170,7 +170,7 @@ extern "C" int balancekv_attn_scored(const void* K, const void* V, const int32_t
   if (const int C = cluster_of(A, n_scored, head_dim, dtype)) {
     e = launch_attn_few_cluster(A, S, C, x, head_dim, dtype, st);
   } else if (A.n_rows <= kFewRows) {
-    e = launch_attn_few(A, x, nullptr, head_dim, dtype, st);
+    e = launch_attn_few(A, x, nullptr, false, head_dim, dtype, st);
     if (e == cudaSuccess && n_scored) e = launch_few_end(A, x, S, head_dim, dtype, st);
     else if (e == cudaSuccess && A.n_slots > 1) e = launch_attn_combine(A, head_dim, dtype, st);
   } else {
@@ -212,14 +212,16 @@ extern "C" int balancekv_decode_attn_prefix(const void* K_prefix, const void* V_
   P.q = A.q = q;
   P.out = A.out = out;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  // Own rows of one split join the prefix's slots themselves (32 sequences behind 32768 rows: 54 us with a launch for that, 45 without).
+  const bool few = prefix_by_few(P, dtype), finish = !few && A.splits == 1 && A.slot0 <= kAttnMaxSplits;
   cudaError_t e;
-  if (prefix_by_few(P, dtype)) {
-    e = launch_attn_few(P, nullptr, A.splits ? &A : nullptr, head_dim, dtype, st);
+  if (few) {
+    e = launch_attn_few(P, nullptr, A.splits ? &A : nullptr, false, head_dim, dtype, st);
   } else {
     e = dtype ? launch_attn_tc(P, head_dim, st) : launch_attn_simt(P, head_dim, dtype, st);
-    if (e == cudaSuccess && A.splits) e = launch_attn_few(A, nullptr, nullptr, head_dim, dtype, st);
+    if (e == cudaSuccess && A.splits) e = launch_attn_few(A, nullptr, nullptr, finish, head_dim, dtype, st);
   }
-  if (e == cudaSuccess && P.n_slots > 1) e = launch_attn_combine(P, head_dim, dtype, st);
+  if (e == cudaSuccess && P.n_slots > 1 && !finish) e = launch_attn_combine(P, head_dim, dtype, st);
   return report("balancekv_decode_attn_prefix", e);
 }
 

@@ -15,6 +15,7 @@
 #include <algorithm>
 #include <climits>
 #include <type_traits>
+#include <utility>
 
 #include "attn_rows.cuh"
 #include "tma_mma.cuh"
@@ -27,6 +28,7 @@ using namespace mma;
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kTile = 32;                        // rows
+constexpr float kGrow = 8.f;                     // a maximum follows when it would grow by more: weights stay below 2^8
 constexpr uint32_t kBox = kTile * 128;           // bytes
 
 template <bool kBf16, int D>
@@ -50,6 +52,7 @@ struct FewJobs {
   FewArgs job[2];
   int32_t groups[2];      // of eight query rows
   int32_t ctas0;          // CTAs of the first set
+  int32_t finish;         // one set of one split: the slots before its own are complete, and it joins them itself
 };
 struct FewMaps {
   CUtensorMap k[2], v[2];
@@ -188,7 +191,8 @@ __device__ inline void few_warp_bf16(const AttnRows& A, const Group& G, const Lo
         for (int tb = 0; tb < 2; ++tb) mma_bf16(sa[tb][k4], ka[k4][tb], qb[kh * 4 + k4][0], qb[kh * 4 + k4][1]);
     }
     R.next(2 * n, lane);
-    float x[2][4], mx[2] = {-INFINITY, -INFINITY};
+    float x[2][4];
+    bool more = false;
 #pragma unroll
     for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
@@ -197,18 +201,15 @@ __device__ inline void few_warp_bf16(const AttnRows& A, const Group& G, const Lo
         const float lw = A.w ? __shfl_sync(0xffffffffu, log_w, in_tile) : 0.f;
         x[tb][j] = row < limit[j & 1] && (alive >> in_tile & 1u) ? fmaf((sa[tb][0][j] + sa[tb][1][j]) + (sa[tb][2][j] + sa[tb][3][j]), A.scale, lw) : -INFINITY;
         if (xs[j & 1] && row < len) xs[j & 1][row] = x[tb][j];
-        mx[j & 1] = fmaxf(mx[j & 1], x[tb][j]);
+        more = more || x[tb][j] > m[j & 1] + kGrow;
       }
-#pragma unroll
-    for (int off = 4; off < 32; off <<= 1) {
-      mx[0] = fmaxf(mx[0], __shfl_xor_sync(0xffffffffu, mx[0], off));
-      mx[1] = fmaxf(mx[1], __shfl_xor_sync(0xffffffffu, mx[1], off));
-    }
-    if (__any_sync(0xffffffffu, mx[0] > m[0] || mx[1] > m[1])) {
+    if (__any_sync(0xffffffffu, more)) {
       float a[2];
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const float mn = fmaxf(m[e], mx[e]);
+        float mn = fmaxf(m[e], fmaxf(fmaxf(x[0][e], x[0][2 + e]), fmaxf(x[1][e], x[1][2 + e])));
+#pragma unroll
+        for (int off = 4; off < 32; off <<= 1) mn = fmaxf(mn, __shfl_xor_sync(0xffffffffu, mn, off));
         a[e] = mn == -INFINITY ? 0.f : exp2f(m[e] - mn);
         l[e] *= a[e];
         m[e] = mn;
@@ -276,13 +277,48 @@ __device__ inline void few_warp_bf16(const AttnRows& A, const Group& G, const Lo
   }
 }
 
-// The same with FFMA; kR >= g rows.  qs: [kR][D], ps: [kR][32] of this warp.
+// The sums over `kG` neighbouring lanes of a[0], .., a[kG - 1], that of a[i] to the lane i of them: kG - 1 exchanges.
+template <int kG>
+__device__ inline float sum_scatter(float (&a)[kG], int lane) {
+#pragma unroll
+  for (int off = kG / 2; off > 0; off /= 2) {
+    const bool upper = lane & off;
+#pragma unroll
+    for (int i = 0; i < off; ++i) {
+      const float give = upper ? a[i] : a[i + off], keep = upper ? a[i + off] : a[i];
+      a[i] = keep + __shfl_xor_sync(0xffffffffu, give, off);
+    }
+  }
+  return a[0];
+}
+
+// The same with FFMA; kR >= g rows.  What bounds it is shared memory, whose loads return 128 bytes a cycle whether lanes read the same or not, so
+// nothing is read that registers can hold.  Logits: kG neighbouring lanes share kG rows of the tile, every lane with a part of the
+// channels of all of them and that part of the queries in registers; a lane ends up with the logit of row `lane`.  Sums: the lanes are kT
+// sets that take every kT-th row, each lane a part of the columns.  (A lane per row with the queries read from shared memory, and all
+// lanes on every row of V: 4300 cycles a tile of d = 64 and four queries.)
+// qs: [kR][D]; ps: [kR][32] of this warp.
 template <int D, int kR>
-__device__ inline void few_warp_fp32(const AttnRows& A, const Group& G, const Logits& X, const Ring<false, D>& R, int s, int len, int n_tiles, int lane, int* abort_flag, const float* qs, float* ps,
-                                     float* mrg, bool& failed) {
+__device__ inline void few_warp_fp32(const AttnRows& A, const Group& G, const Logits& X, const Ring<false, D>& R, int s, int len, int n_tiles, int lane, int* abort_flag,
+                                     const float* qs, float* ps, float* mrg, bool& failed) {
   const int g = G.g;
-  constexpr int kC = D / 32;                     // columns of a lane: kC lane ..
-  float o[kR][kC], m[kR], l[kR];
+  constexpr int kAtOnce = kR < 4 ? kR : 4;       // queries whose logits are formed together; of more, they come from shared memory for each tile
+  constexpr int kG = kAtOnce * D / 4 <= 64 ? 4 : 8, kPieces = D / 4 / kG;      // 16-byte pieces of a row that a lane takes: its number + kG c
+  constexpr int kT = kR * D / 8 <= 64 ? 4 : 2, kLanes = 32 / kT, kC = D / 4 / kLanes;
+  float2 q[kAtOnce][kPieces][2];
+  auto ask = [&](int r0) {                       // the queries r0 .. r0 + kAtOnce - 1
+#pragma unroll
+    for (int r = 0; r < kAtOnce; ++r)
+#pragma unroll
+      for (int c = 0; c < kPieces; ++c) {
+        const float4 w = *reinterpret_cast<const float4*>(qs + (r0 + r) * D + 4 * (lane % kG + kG * c));
+        q[r][c][0] = make_float2(w.x, w.y);
+        q[r][c][1] = make_float2(w.z, w.w);
+      }
+  };
+  if (kR <= kAtOnce) ask(0);
+  float2 o[kR][kC][2];
+  float m[kR], l[kR];
   int limit[kR];
 #pragma unroll
   for (int r = 0; r < kR; ++r) {
@@ -290,8 +326,11 @@ __device__ inline void few_warp_fp32(const AttnRows& A, const Group& G, const Lo
     l[r] = 0.f;
     limit[r] = r < g ? attn_limit(A, len, G.r0 + r) : 0;
 #pragma unroll
-    for (int c = 0; c < kC; ++c) o[r][c] = 0.f;
+    for (int c = 0; c < kC; ++c) o[r][c][0] = o[r][c][1] = make_float2(0.f, 0.f);
   }
+  // piece c of this lane's columns: box and place of it
+  const int set = lane / kLanes, in_set = lane % kLanes;
+  auto piece = [&](int c) { return (in_set & 7) + 8 * ((in_set >> 3) + c * (kLanes / 8)); };
   TileWeights W{A.w ? A.w + (int64_t)s * A.cap : nullptr};
   W.ask(R.first_tile * kTile + lane, len);
   for (int n = 0; n < n_tiles; ++n) {
@@ -301,28 +340,38 @@ __device__ inline void few_warp_fp32(const AttnRows& A, const Group& G, const Lo
     W.ask(row + kWarps * kTile, len);
     if (!R.wait(2 * n, lane, abort_flag)) { R.drain(2 * n, lane); failed = true; break; }
     const unsigned char* Kt = R.at(2 * n);
-    float2 acc[kR];
-#pragma unroll
-    for (int r = 0; r < kR; ++r) acc[r] = make_float2(0.f, 0.f);
-#pragma unroll 4
-    for (int c = 0; c < D / 4; ++c) {
-      const float4 k = *reinterpret_cast<const float4*>(Kt + tile_off(lane, c));
-#pragma unroll
-      for (int r = 0; r < kR; ++r) {
-        const float4 q = *reinterpret_cast<const float4*>(qs + r * D + 4 * c);
-        acc[r] = __ffma2_rn(make_float2(k.x, k.y), make_float2(q.x, q.y), acc[r]);
-        acc[r] = __ffma2_rn(make_float2(k.z, k.w), make_float2(q.z, q.w), acc[r]);
-      }
-    }
-    R.next(2 * n, lane);
     float x[kR];
     bool more = false;
 #pragma unroll
-    for (int r = 0; r < kR; ++r) {
-      x[r] = row < limit[r] && (alive >> lane & 1u) ? fmaf(acc[r].x + acc[r].y, A.scale, log_w) : -INFINITY;
-      if (X.x && r < g && row < len) X.x[r * X.pitch + row] = x[r];
-      more = more || x[r] > m[r];
+    for (int r0 = 0; r0 < kR; r0 += kAtOnce) {
+      if (kR > kAtOnce) ask(r0);
+      float part[kAtOnce][kG];
+#pragma unroll
+      for (int i = 0; i < kG; ++i) {
+        float2 acc[kAtOnce];
+#pragma unroll
+        for (int r = 0; r < kAtOnce; ++r) acc[r] = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int c = 0; c < kPieces; ++c) {
+          const float4 k = *reinterpret_cast<const float4*>(Kt + tile_off((lane & ~(kG - 1)) + i, lane % kG + kG * c));
+#pragma unroll
+          for (int r = 0; r < kAtOnce; ++r) {
+            acc[r] = __ffma2_rn(make_float2(k.x, k.y), q[r][c][0], acc[r]);
+            acc[r] = __ffma2_rn(make_float2(k.z, k.w), q[r][c][1], acc[r]);
+          }
+        }
+#pragma unroll
+        for (int r = 0; r < kAtOnce; ++r) part[r][i] = acc[r].x + acc[r].y;
+      }
+#pragma unroll
+      for (int r = r0; r < r0 + kAtOnce; ++r) {
+        const float dot = sum_scatter<kG>(part[r - r0], lane);
+        x[r] = row < limit[r] && (alive >> lane & 1u) ? fmaf(dot, A.scale, log_w) : -INFINITY;
+        if (X.x && r < g && row < len) X.x[r * X.pitch + row] = x[r];
+        more = more || x[r] > m[r] + kGrow;
+      }
     }
+    R.next(2 * n, lane);
     if (__any_sync(0xffffffffu, more)) {
 #pragma unroll
       for (int r = 0; r < kR; ++r) {
@@ -330,57 +379,44 @@ __device__ inline void few_warp_fp32(const AttnRows& A, const Group& G, const Lo
         m[r] = mn;
         l[r] *= a;
 #pragma unroll
-        for (int c = 0; c < kC; ++c) o[r][c] *= a;
+        for (int c = 0; c < kC; ++c) {
+          o[r][c][0] = __fmul2_rn(o[r][c][0], make_float2(a, a));
+          o[r][c][1] = __fmul2_rn(o[r][c][1], make_float2(a, a));
+        }
       }
     }
 #pragma unroll
     for (int r = 0; r < kR; ++r) {
       const float p = exp2f(x[r] - (m[r] == -INFINITY ? 0.f : m[r]));
       l[r] += p;
-      ps[r * 32 + lane] = p;
+      ps[r * 32 + lane % kT * kLanes + lane / kT] = p;     // a set's rows next to one another
     }
     if (!R.wait(2 * n + 1, lane, abort_flag)) { R.drain(2 * n + 1, lane); failed = true; break; }        // (a warp barrier too: the weights are there)
     const unsigned char* Vt = R.at(2 * n + 1);
-    auto value = [&](int t, float (&v)[kC]) {
-      const unsigned char* at = Vt + tile_off(t, lane * kC / 4) + (lane * kC % 4) * 4;
-      if constexpr (kC == 4) {
-        const float4 w = *reinterpret_cast<const float4*>(at);
-        v[0] = w.x; v[1] = w.y; v[2] = w.z; v[3] = w.w;
-      } else {
-        const float2 w = *reinterpret_cast<const float2*>(at);
-        v[0] = w.x; v[1] = w.y;
-      }
-    };
-    auto add = [&](const float (&v)[kC], int r, float p) {
 #pragma unroll
-      for (int c = 0; c < kC; c += 2) {
-        const float2 y = __ffma2_rn(make_float2(v[c], v[c + 1]), make_float2(p, p), make_float2(o[r][c], o[r][c + 1]));
-        o[r][c] = y.x;
-        o[r][c + 1] = y.y;
-      }
-    };
-    if (alive == 0xffffffffu) {
-#pragma unroll 2
-      for (int t = 0; t < kTile; t += 4) {
-        float v[4][kC];
+    for (int t0 = 0; t0 < kLanes; t0 += 4) {               // the set's rows t0 .. t0 + 3
+      float4 v[4][kC];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) value(t + i, v[i]);
+      for (int i = 0; i < 4; ++i) {
+        const int t = (t0 + i) * kT + set;
 #pragma unroll
-        for (int r = 0; r < kR; ++r) {
-          const float4 p = *reinterpret_cast<const float4*>(ps + r * 32 + t);
-          add(v[0], r, p.x);
-          add(v[1], r, p.y);
-          add(v[2], r, p.z);
-          add(v[3], r, p.w);
+        for (int c = 0; c < kC; ++c) v[i][c] = *reinterpret_cast<const float4*>(Vt + tile_off(t, piece(c)));
+        if (alive != 0xffffffffu && !(alive >> t & 1u)) {  // does not count: what it holds may be anything
+#pragma unroll
+          for (int c = 0; c < kC; ++c) v[i][c] = make_float4(0.f, 0.f, 0.f, 0.f);
         }
       }
-    } else {
-      for (int t = 0; t < kTile; ++t) {
-        if (!(alive >> t & 1u)) continue;        // does not count: what it holds may be anything
-        float v[kC];
-        value(t, v);
 #pragma unroll
-        for (int r = 0; r < kR; ++r) add(v, r, ps[r * 32 + t]);
+      for (int r = 0; r < kR; ++r) {
+        const float4 p4 = *reinterpret_cast<const float4*>(ps + r * 32 + set * kLanes + t0);
+        const float p[4] = {p4.x, p4.y, p4.z, p4.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int c = 0; c < kC; ++c) {
+            o[r][c][0] = __ffma2_rn(make_float2(v[i][c].x, v[i][c].y), make_float2(p[i], p[i]), o[r][c][0]);
+            o[r][c][1] = __ffma2_rn(make_float2(v[i][c].z, v[i][c].w), make_float2(p[i], p[i]), o[r][c][1]);
+          }
       }
     }
     R.next(2 * n + 1, lane);
@@ -388,12 +424,18 @@ __device__ inline void few_warp_fp32(const AttnRows& A, const Group& G, const Lo
   __syncthreads();
 #pragma unroll
   for (int r = 0; r < kR; ++r) {
-    if (r >= g) break;
+    const float sum = warp_sum(l[r]);
     float* to = mrg + r * Few<false, D>::kPitch;
 #pragma unroll
-    for (int c = 0; c < kC; ++c) to[lane * kC + c] = o[r][c];
-    const float sum = warp_sum(l[r]);
-    if (lane == 0) { to[D] = m[r]; to[D + 1] = sum; }
+    for (int c = 0; c < kC; ++c) {
+      float w[4] = {o[r][c][0].x, o[r][c][0].y, o[r][c][1].x, o[r][c][1].y};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int off = kLanes; off < 32; off <<= 1) w[i] += __shfl_xor_sync(0xffffffffu, w[i], off);
+      if (r < g && set == 0) *reinterpret_cast<float4*>(to + 4 * piece(c)) = make_float4(w[0], w[1], w[2], w[3]);
+    }
+    if (r < g && lane == 0) { to[D] = m[r]; to[D + 1] = sum; }
   }
 }
 
@@ -429,8 +471,10 @@ __device__ inline void few_tiles(const AttnRows& A, const Group& G, const Logits
 }
 
 template <bool kBf16, int D, int kR>
-__device__ inline void few_init(FewShared<kBf16, D, kR>& sh) {
+__device__ inline void few_init(FewShared<kBf16, D, kR>& sh, const CUtensorMap& mk, const CUtensorMap& mv) {
   if (threadIdx.x != 0) return;
+  asm volatile("prefetch.tensormap [%0];" ::"l"(&mk) : "memory");
+  asm volatile("prefetch.tensormap [%0];" ::"l"(&mv) : "memory");
   for (int i = 0; i < kWarps * Few<kBf16, D>::kRing; ++i) tc::mbar_init(&sh.full[0][0] + i, 1);
   sh.abort_flag = 0;
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -483,6 +527,53 @@ __device__ inline void few_put(const AttnRows& A, int64_t row, int lane, const f
   }
 }
 
+// A row's sums and those of the slots before its own, by a warp.
+template <int D>
+__device__ inline void join_before(const AttnRows& A, int64_t row, int lane, float (&acc)[D / 32], float top, float& sum) {
+  constexpr int kC = D / 32, kChunks = kAttnMaxSplits / 32, kAhead = 6;
+  float2 ml[kChunks];
+  float most = top, f[kChunks];
+#pragma unroll
+  for (int k = 0; k < kChunks; ++k) {
+    ml[k] = lane + 32 * k < A.slot0 ? A.part_ml[(int64_t)(lane + 32 * k) * A.total_rows + row] : make_float2(-INFINITY, 0.f);
+    most = fmaxf(most, ml[k].x);
+  }
+  most = warp_max(most);
+  const float base = most == -INFINITY ? 0.f : most, own = exp2f(top - base);
+  float rest = 0.f;
+#pragma unroll
+  for (int k = 0; k < kChunks; ++k) {
+    f[k] = exp2f(ml[k].x - base);
+    rest = fmaf(ml[k].y, f[k], rest);
+  }
+  sum = fmaf(sum, own, warp_sum(rest));
+#pragma unroll
+  for (int c = 0; c < kC; ++c) acc[c] *= own;
+#pragma unroll
+  for (int k = 0; k < kChunks; ++k)
+    for (int i0 = 32 * k; i0 < min(32 * k + 32, A.slot0); i0 += kAhead) {
+      float v[kAhead][kC];
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        const float* from = A.part + ((int64_t)(i0 + j) * A.total_rows + row) * D + lane * kC;
+        const bool in = i0 + j < min(32 * k + 32, A.slot0);
+#pragma unroll
+        for (int c = 0; c < kC; c += 2) {
+          const float2 x = in ? *reinterpret_cast<const float2*>(from + c) : make_float2(0.f, 0.f);
+          v[j][c] = x.x;
+          v[j][c + 1] = x.y;
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        if (i0 + j >= min(32 * k + 32, A.slot0)) break;
+        const float w = __shfl_sync(0xffffffffu, f[k], i0 + j & 31);
+#pragma unroll
+        for (int c = 0; c < kC; ++c) acc[c] = fmaf(v[j][c], w, acc[c]);
+      }
+    }
+}
+
 // kR: rows that the fp32 form takes (bf16: 8).
 template <bool kBf16, int D, int kR>
 __global__ void __launch_bounds__(kThreads, (Few<kBf16, D>::kCtas)) attn_few_kernel(const __grid_constant__ FewJobs J, const __grid_constant__ FewMaps maps) {
@@ -496,7 +587,7 @@ __global__ void __launch_bounds__(kThreads, (Few<kBf16, D>::kCtas)) attn_few_ker
   // the groups of a stream's query rows next to one another: they read the same rows
   const int group = cta % J.groups[which], split = cta / J.groups[which] % A.splits, s = cta / J.groups[which] / A.splits;
   const Group G{group * kFewRows, min(kFewRows, A.n_rows - group * kFewRows)};
-  few_init(sh);
+  few_init(sh, maps.k[which], maps.v[which]);
   grid_wait_and_release();
   __syncthreads();
   const int len = attn_len(A, s), n_all = (len + kTile - 1) / kTile;
@@ -509,6 +600,11 @@ __global__ void __launch_bounds__(kThreads, (Few<kBf16, D>::kCtas)) attn_few_ker
     few_join<D, kWarps>(kWarps, lane, [&](int w) { return mrg + (w * kFewRows + r) * F::kPitch; }, acc, top, sum);
     if (sh.abort_flag) sum = NAN;
     const int64_t row = attn_row(A, s, G.r0 + r);
+    if (J.finish) {
+      join_before<D>(A, row, lane, acc, top, sum);
+      few_put<kBf16, D>(A, row, lane, acc, sum);
+      continue;
+    }
     if (A.n_slots > 1) {
       const int64_t at = (int64_t)(A.slot0 + split) * A.total_rows + row;
       if (lane == 0) A.part_ml[at] = make_float2(top, sum);
@@ -542,7 +638,7 @@ attn_few_cluster_kernel(const __grid_constant__ AttnRows A, const ScoreArgs S, i
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
   const int C = (int)gridDim.y, c = blockIdx.y, s = blockIdx.x % A.n_streams, group = blockIdx.x / A.n_streams;
   const Group G{group * kFewRows, min(kFewRows, A.n_rows - group * kFewRows)};
-  few_init(sh);
+  few_init(sh, mk, mv);
   grid_wait_and_release();
   __syncthreads();
   const int len = attn_len(A, s), n_all = (len + kTile - 1) / kTile;
@@ -559,30 +655,48 @@ attn_few_cluster_kernel(const __grid_constant__ AttnRows A, const ScoreArgs S, i
     for (int i = 0; i < D / 32; ++i) to[lane * (D / 32) + i] = acc[i];
     if (lane == 0) { to[D] = top; to[D + 1] = sum; }
   }
+  // The old scores of this CTA's rows, the first kOld per thread, on their way while the cluster meets.
+  constexpr int kOld = 4;
+  const int64_t first = (int64_t)s * A.cap;
+  float old[kOld];
+#pragma unroll
+  for (int j = 0; j < kOld; ++j) old[j] = !sums && row0 + tid + j * kThreads < row1 ? score_old(S, first + row0 + tid + j * kThreads) : 0.f;
   cluster.sync();
-  // The rows' sums over the cluster: a lane per CTA.
-  for (int r = warp; r < G.g; r += kWarps) {
+  // The rows' sums over the cluster, a lane per CTA: two rows of every warp's, asked for together.
+  static_assert(kFewRows <= 2 * kWarps, "two rows a warp");
+  float2 ml[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int r = warp + i * kWarps;
     const float* at = cluster.map_shared_rank(joined, lane < C ? lane : 0) + r * F::kPitch;
-    const float m = lane < C ? at[D] : -INFINITY, l = lane < C ? at[D + 1] : 0.f;
-    const float top = warp_max(m), base = top == -INFINITY ? 0.f : top, sum = warp_sum(l * exp2f(m - base));
-    const bool counted = (G.r0 + r) % A.n_queries >= A.n_queries - S.n_scored;
-    if (lane == 0) lse[r] = sum == 0.f || !counted ? INFINITY : base + log2f(sum);
+    ml[i] = lane < C && r < G.g ? make_float2(at[D], at[D + 1]) : make_float2(-INFINITY, 0.f);
   }
-  // The outputs: row r by the warp r of the cluster's.
-  for (int r = c + C * warp; r < G.g; r += C * kWarps) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int r = warp + i * kWarps;
+    const float top = warp_max(ml[i].x), base = top == -INFINITY ? 0.f : top, sum = warp_sum(ml[i].y * exp2f(ml[i].x - base));
+    const bool counted = (G.r0 + r) % A.n_queries >= A.n_queries - S.n_scored;
+    if (lane == 0 && r < G.g) lse[r] = sum == 0.f || !counted ? INFINITY : base + log2f(sum);
+  }
+  // The outputs: a warp of the cluster's each, the last warps first.
+  for (int r = c + C * (kWarps - 1 - warp); r < G.g; r += C * kWarps) {
     float acc[D / 32], top, sum;
     few_join<D, kMaxCluster>(C, lane, [&](int b) { return cluster.map_shared_rank(joined, b) + r * F::kPitch; }, acc, top, sum);
     few_put<kBf16, D>(A, attn_row(A, s, G.r0 + r), lane, acc, sum);
   }
   __syncthreads();
-  const int64_t first = (int64_t)s * A.cap;
-  for (int i = row0 + tid; i < row1; i += kThreads) {
+  auto left = cluster.barrier_arrive();          // this CTA reads nobody's sums any more
+  auto put = [&](int i, float before) {
     float sum = 0.f;
     for (int r = 0; r < G.g; ++r) sum += exp2f(x[r * pitch + i - row0] - lse[r]);
     if (sums) sums[(int64_t)group * A.n_streams * A.cap + first + i] = sum;
-    else score_put(S, first + i, sum);
-  }
-  cluster.sync();                                // nobody reads this CTA's sums any more
+    else score_put(S, first + i, before, sum);
+  };
+#pragma unroll
+  for (int j = 0; j < kOld; ++j)
+    if (row0 + tid + j * kThreads < row1) put(row0 + tid + j * kThreads, old[j]);
+  for (int i = row0 + tid + kOld * kThreads; i < row1; i += kThreads) put(i, sums ? 0.f : score_old(S, first + i));
+  cluster.barrier_wait(std::move(left));         // nobody reads this CTA's
 }
 
 // The scores from the groups' sums.
@@ -672,9 +786,10 @@ cudaError_t for_rows(int n_rows, Run run) {
 }
 
 template <bool kBf16, int D>
-cudaError_t launch_few(const FewArgs& P, const FewArgs* also, cudaStream_t st) {
+cudaError_t launch_few(const FewArgs& P, const FewArgs* also, bool finish, cudaStream_t st) {
   using F = Few<kBf16, D>;
   FewJobs J{};
+  J.finish = finish;
   FewMaps maps;
   int64_t ctas = 0;
   int most = 0;
@@ -766,10 +881,11 @@ int64_t few_cluster_sums(const AttnRows& A) { return A.n_rows > kFewRows ? (int6
 int64_t few_pitch(int cap) { return ((int64_t)cap + 31) / 32 * 32; }
 
 // x: [n_streams, n_rows, few_pitch(cap)] where launch_few_end is to follow, else null.  `also`: a second set of streams of the same call.
-cudaError_t launch_attn_few(const AttnRows& A, float* x, const AttnRows* also, int d, int is_bf16, cudaStream_t st) {
+// finish (one split): the outputs, joined with the slots of the launches before.
+cudaError_t launch_attn_few(const AttnRows& A, float* x, const AttnRows* also, bool finish, int d, int is_bf16, cudaStream_t st) {
   const FewArgs P{A, x, few_pitch(A.cap)}, Q{also ? *also : A, nullptr, 0}, *second = also ? &Q : nullptr;
-  if (is_bf16) return d == 128 ? launch_few<true, 128>(P, second, st) : launch_few<true, 64>(P, second, st);
-  return d == 128 ? launch_few<false, 128>(P, second, st) : launch_few<false, 64>(P, second, st);
+  if (is_bf16) return d == 128 ? launch_few<true, 128>(P, second, finish, st) : launch_few<true, 64>(P, second, finish, st);
+  return d == 128 ? launch_few<false, 128>(P, second, finish, st) : launch_few<false, 64>(P, second, finish, st);
 }
 
 // Outputs and scores by clusters of C CTAs.

@@ -70,7 +70,8 @@ def test_one_query(cuda_lib, dtype, d, g, cap, lens):
     (128, 4, 300, [300, 299, 128, 1, 0], 128, 128), (64, 2, 1000, [1000, 33, 32, 5, 517], 33, 33), (128, 1, 129, [129, 128, 127], 129, 64),
     (64, 3, 513, [513, 400, 100], 200, 1), (128, 8, 70, [70, 3], 2, 2), (128, 5, 2000, [2000, 1999], 3, 3), (64, 4, 640, [640], 640, 640),
     (128, 4, 1300, [1300, 1217], 257, 100), (128, 3, 4200, [4200, 4095], 65, 65), (64, 8, 900, [900, 130, 131], 130, 7), (128, 2, 512, [512, 256], 256, 256),
-    (128, 6, 385, [385, 384, 383, 200], 384, 130), (64, 1, 2300, [2300, 1150], 1150, 1150),
+    (128, 6, 385, [385, 384, 383, 200], 384, 130), (64, 1, 2300, [2300, 1150], 1150, 1150), (128, 8, 700, [700, 650], 300, 9), (128, 7, 500, [500, 260], 260, 33),
+    (64, 5, 400, [400, 399, 100], 150, 64), (128, 8, 330, [330], 330, 1), (128, 8, 1030, [1030, 1024], 1024, 1024),
 ])
 def test_many_queries(cuda_lib, dtype, d, g, cap, lens, m, n_scored):
     _check_scored(cuda_lib, dtype, d, g, cap, lens, m, n_scored, seed=m)
