@@ -16,6 +16,16 @@ constexpr int kTcRows = 128, kTcKeys = 128;      // a tile of logits
 __device__ inline uint32_t umma_desc_lo_outer(uint32_t smem_addr, uint32_t lead) { return ((smem_addr & 0x3FFFFu) >> 4) | ((lead >> 4) << 16); }
 constexpr uint32_t kOuterB = 1u << 16;           // instruction descriptor: B is laid out so
 
+// D[128][N] (+)= A[128][16] B[N][16], both from shared memory, N by the instruction descriptor.
+__device__ inline void umma_n(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t instr, bool accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "mov.b64 da, {%1, %3};\n\t"
+      "mov.b64 db, {%2, %3};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %5, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(kDescHi), "r"((uint32_t)accumulate), "r"(instr) : "memory");
+}
 // D[128][N] (+)= A[128][16] B[16][N] with A in TMEM, two bf16 to a column.
 template <uint32_t kInstr>
 __device__ inline void umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, bool accumulate) {

@@ -859,11 +859,11 @@ cudaError_t launch_end(const FewArgs& P, const ScoreArgs& S, cudaStream_t st) {
 }  // namespace
 
 // Split factor of the kernels above: as many CTAs as fit the SMs at once, with a tile for each warp; and of long caches, in parts of 1024
-// rows, up to four times as many, so that streams of different lengths even out.
+// rows, up to six times as many, so that streams of different lengths even out (256 streams of up to 8192 rows: 104.9 us by 5 splits, 102.2 by 7).
 int few_splits(int64_t streams, int cap, int n_rows) {
   const int64_t sets = streams * ((n_rows + kFewRows - 1) / kFewRows);
   const int64_t fill = std::min<int64_t>(2 * kAttnSms / sets, (cap + kWarps * kTile - 1) / (kWarps * kTile));
-  const int64_t even = std::min<int64_t>((8 * kAttnSms + sets - 1) / sets, cap / 1024);
+  const int64_t even = std::min<int64_t>((12 * kAttnSms + sets - 1) / sets, cap / 1024);
   return (int)std::max<int64_t>(1, std::min<int64_t>(std::max(fill, even), kAttnMaxSplits));
 }
 

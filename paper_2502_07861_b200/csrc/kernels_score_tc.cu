@@ -7,7 +7,7 @@
 // adds up one row's weights and no sum crosses threads.
 //
 // A CTA keeps 128 cached rows in shared memory and walks the queries in tiles of 128, head by head, from the first tile that sees its
-// rows on; where at most 64 queries count, a tile has several heads'.  Two warpgroups take half of a tile's queries each, from two
+// rows on; where at most 64 queries of more heads count, a tile has several heads'.  Two warpgroups take half of a tile's queries each, from two
 // buffers of 128 x 128 logits in TMEM.  Two CTAs share an SM, so that the start of one runs under the other's tiles.  (One CTA of 256 rows:
 // 64 of 2048 queries of 4 heads over 8 x 32768 rows took 67 us.)  Where there are few CTAs the tiles are shared out to a cluster, whose
 // sums meet in shared memory.
@@ -16,6 +16,9 @@
 // Warps: 0-7 the rows, 8 asks for K and the Q tiles (TMA) and loads their lse, 9 issues the MMAs.
 // Every wait is bounded; one that gives up makes the scores NaN.
 #include <cooperative_groups.h>
+
+#include <algorithm>
+#include <type_traits>
 
 #include "attn_tc.cuh"
 
@@ -248,14 +251,202 @@ score_tc_kernel(const __grid_constant__ AttnRows A, const ScoreArgs C, int box_r
   if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(256u) : "memory");
 }
 
+// The same where the counted queries of a stream fill one or two tiles: they stay in shared memory and the cached rows go by, a CTA's
+// share of the stream's tiles of 128 rows.  A tile of queries has `cols` rows, as few 32s as hold its heads' boxes: the products and
+// exponentials of the others are saved.  Warps as above; every tile's rows are added up over the two warpgroups and written at once.
+template <int D>
+struct StreamShape {
+  static constexpr uint32_t kBox = 128 * 128;
+  static constexpr uint32_t kTile = (D / 64) * kBox;
+  static constexpr int kRing = D == 128 ? 4 : 8;
+  static constexpr size_t kSmem = 1024 + (2 + kRing) * (size_t)kTile;
+};
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+score_stream_kernel(const __grid_constant__ AttnRows A, const ScoreArgs C, int box_rows, int q_tiles, int cols, const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk) {
+  using Sh = StreamShape<D>;
+  constexpr int kRing = Sh::kRing;
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ uint64_t q_full, k_full[kRing], k_empty[kRing], s_full[4], s_empty[4], drained;
+  __shared__ uint32_t tmem_s;
+  __shared__ int abort_flag;
+  __shared__ __align__(16) float lse[2][kTcRows];             // negative
+  __shared__ __align__(16) int query[2][kTcRows];             // of a head
+  __shared__ float total[2][kTcKeys];            // the second warpgroup's sums of a tile
+  unsigned char* sm = smem_raw + (-smem_u32(smem_raw) & 1023u);
+  unsigned char* ring = sm + 2 * Sh::kTile;
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid / 32, 0), lane = tid % 32;
+  const int pack = kTcRows / box_rows;           // heads of a tile
+  if (tid == 0) {
+    mbar_init(&q_full, 1);
+    mbar_init(&drained, 1);
+    for (int i = 0; i < kRing; ++i) { mbar_init(k_full + i, 1); mbar_init(k_empty + i, 1); }
+    for (int i = 0; i < 4; ++i) { mbar_init(s_full + i, 1); mbar_init(s_empty + i, 256); }
+    abort_flag = 0;
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&mq) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&mk) : "memory");
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (box_rows < kTcRows)                        // what no head's queries fill is zero, so that its weights are
+    for (int i = tid; i < 2 * (int)Sh::kTile / 16; i += kThreads) reinterpret_cast<uint4*>(sm)[i] = make_uint4(0, 0, 0, 0);
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  if (warp == 9) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_s)), "r"(512u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  grid_wait_and_release();
+  const int s = blockIdx.x, len = attn_len(A, s), m = A.n_queries, heads = A.n_rows / m, start = m - C.n_scored;
+  const int all = (len + kTcKeys - 1) / kTcKeys;
+  const int t0 = (int)((int64_t)all * blockIdx.y / gridDim.y), n = (int)((int64_t)all * (blockIdx.y + 1) / gridDim.y) - t0;      // this CTA's
+  // query row r of tile t: head and query (box_rows = 128: a head to a tile)
+  if (n > 0)
+    for (int i = tid; i < 2 * kTcRows; i += kThreads) {
+      const int t = i / kTcRows, r = i % kTcRows, h = t * pack + r / box_rows, q = start + r % box_rows;
+      lse[t][r] = t < q_tiles && r < pack * box_rows && h < heads && q < m ? -A.lse[((int64_t)s * heads + h) * m + q] : -INFINITY;
+      query[t][r] = q;
+    }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_s, 0);
+
+  if (warp == 8 && n > 0) {
+    bool ok = true;
+    if (lane == 0) {
+      mbar_expect_tx(&q_full, (uint32_t)heads * box_rows * 2 * D);
+      for (int h = 0; h < heads; ++h)
+        for (int b = 0; b < D / 64; ++b)
+          tma_load_3d(sm + h / pack * Sh::kTile + b * Sh::kBox + h % pack * box_rows * 128, &mq, 64 * b, start, s * heads + h, &q_full);
+    }
+    int i = 0;
+    for (; i < n; ++i) {
+      const int slot = i % kRing;
+      if (i >= kRing) ok = wait_bar(k_empty + slot, (uint32_t)(i / kRing - 1) & 1u, &abort_flag);
+      if (!__all_sync(0xffffffffu, ok)) break;
+      if (lane == 0) {
+        mbar_expect_tx(k_full + slot, Sh::kTile);
+        for (int b = 0; b < D / 64; ++b) tma_load_3d(ring + slot * Sh::kTile + b * Sh::kBox, &mk, 64 * b, (t0 + i) * kTcKeys, s, k_full + slot);
+      }
+      __syncwarp();
+    }
+    if (i < n && lane == 0) {                    // gave up: the copies in flight, within limits
+      const long long w0 = clock64();
+      while (!mbar_try_wait(&q_full, 0) && clock64() - w0 < kWaitCycles) {}
+      for (int e = max(0, i - kRing); e < i; ++e)
+        while (!mbar_try_wait(k_full + e % kRing, (uint32_t)(e / kRing) & 1u) && clock64() - w0 < kWaitCycles) {}
+    }
+  } else if (warp == 9 && n > 0) {
+    bool ok = true;
+    auto wait = [&](uint64_t* bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, wait_bar(bar, parity, &abort_flag)); };
+    const uint32_t instr = (kInstrBf16<kTcRows> & ~(63u << 17)) | (uint32_t)(cols >> 3) << 17;
+    wait(&q_full, 0);
+    int u = 0;                                   // products so far: the buffer u % 4 of logits
+    for (int i = 0; i < n && ok; ++i) {
+      wait(k_full + i % kRing, (uint32_t)(i / kRing) & 1u);
+      for (int t = 0; t < q_tiles; ++t, ++u) {
+        if (u > 3) wait(s_empty + (u & 3), (uint32_t)(u / 4 - 1) & 1u);
+        tc_fence_after();
+        if (ok && elect_one()) {
+          const uint32_t a = umma_desc_lo(smem_u32(ring + i % kRing * Sh::kTile)), b = umma_desc_lo(smem_u32(sm + t * Sh::kTile)), d = tmem + 128 * (u & 3);
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k) {
+            const uint32_t at = (uint32_t)(k / 4) * (Sh::kBox >> 4) + 2 * (k % 4);
+            umma_n(d, a + at, b + at, instr, k > 0);
+          }
+          umma_commit(s_full + (u & 3));
+          if (t == q_tiles - 1) umma_commit(k_empty + i % kRing);
+        }
+        __syncwarp();
+      }
+    }
+    if (!ok) {                                   // gave up: the products in flight, within limits
+      if (elect_one()) umma_commit(&drained);
+      st_release(&abort_flag, 1);
+      const long long w0 = clock64();
+      while (!mbar_try_wait(&drained, 0) && clock64() - w0 < kWaitCycles) {}
+    }
+  } else if (warp < 8) {
+    const int h = warp / 4, lanes = 32 * (warp % 4);
+    const uint32_t S = tmem + ((uint32_t)lanes << 16);
+    const float2 scale2 = make_float2(A.scale, A.scale);
+    bool ok = true;
+    int u = 0;
+    for (int i = 0; i < n; ++i) {
+      const int key0 = (t0 + i) * kTcKeys, key = key0 + lanes + lane, from = key - (len - m);      // the first query that sees the row
+      const int64_t at = (int64_t)s * A.cap + key;
+      const float old = h == 0 && key < len ? score_old(C, at) : 0.f;
+      const bool masked = key0 + kTcKeys - 1 > len - m + start;
+      float2 part[2] = {};
+      for (int t = 0; t < q_tiles; ++t, ++u) {
+        ok = ok && __all_sync(0xffffffffu, wait_bar(s_full + (u & 3), (uint32_t)(u / 4) & 1u, &abort_flag));
+        if (!ok) break;
+        tc_fence_after();
+        for (int c = 32 * h; c < cols; c += 64) {          // the warpgroups take 32 columns in turn
+          float x[32];
+          tmem_ld32(S + 128 * (u & 3) + c, x);
+          tmem_ld_wait();
+          const float4* l4 = reinterpret_cast<const float4*>(lse[t] + c);
+          const int4* q4 = reinterpret_cast<const int4*>(query[t] + c);
+          auto weights = [&](auto mask) {
+#pragma unroll
+            for (int k = 0; k < 32; k += 4) {
+              const float4 l = l4[k / 4];
+              const float2 lo = __ffma2_rn(make_float2(x[k], x[k + 1]), scale2, make_float2(l.x, l.y));
+              const float2 hi = __ffma2_rn(make_float2(x[k + 2], x[k + 3]), scale2, make_float2(l.z, l.w));
+              float2 a = make_float2(ex2(lo.x), ex2(lo.y)), b = make_float2(ex2(hi.x), ex2(hi.y));
+              if constexpr (decltype(mask)::value) {
+                const int4 q = q4[k / 4];
+                a = make_float2(q.x >= from ? a.x : 0.f, q.y >= from ? a.y : 0.f);
+                b = make_float2(q.z >= from ? b.x : 0.f, q.w >= from ? b.y : 0.f);
+              }
+              part[0] = __fadd2_rn(part[0], a);
+              part[1] = __fadd2_rn(part[1], b);
+            }
+          };
+          if (masked) weights(std::true_type{});
+          else weights(std::false_type{});
+        }
+        tc_fence_before();
+        mbar_arrive(s_empty + (u & 3));
+      }
+      float sum = ok ? (part[0].x + part[0].y) + (part[1].x + part[1].y) : NAN;
+      if (h == 1) total[i & 1][lanes + lane] = sum;
+      asm volatile("bar.sync 1, 256;" ::: "memory");       // the row warps; the place is written again behind the next tile's barrier
+      if (h == 0 && key < len) score_put(C, at, old, sum + total[i & 1][lanes + lane]);
+    }
+    tc_fence_before();
+  }
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+}
+
+template <int D>
+cudaError_t launch_stream(const AttnRows& A, const ScoreArgs& S, int box_rows, const CUtensorMap& mq, const CUtensorMap& mk, cudaStream_t st) {
+  static std::atomic<unsigned long long> devices{0};
+  const cudaError_t e = kernel_limits(score_stream_kernel<D>, StreamShape<D>::kSmem, false, devices);
+  if (e != cudaSuccess) return e;
+  const int heads = A.n_rows / A.n_queries, pack = kTcRows / box_rows, q_tiles = (heads + pack - 1) / pack;
+  const int cols = (std::min(heads, pack) * box_rows + 31) / 32 * 32;
+  // a CTA an SM, or two waves of them where the streams alone are more, with four tiles each while that leaves none idle
+  const int64_t tiles = (A.cap + kTcKeys - 1) / kTcKeys;
+  const int64_t parts = std::max<int64_t>(1, std::min<int64_t>((A.n_streams > kAttnSms ? 4 : 1) * kAttnSms / A.n_streams, tiles));
+  const PdlConfig pc(dim3((unsigned)A.n_streams, (unsigned)parts), kThreads, StreamShape<D>::kSmem, st);
+  return cudaLaunchKernelEx(&pc.cfg, score_stream_kernel<D>, A, S, box_rows, q_tiles, cols, mq, mk);
+}
+
 template <int D>
 cudaError_t launch(const AttnRows& A, const ScoreArgs& S, cudaStream_t st) {
   CUtensorMap mq, mk;
   const int box_rows = S.n_scored > 64 ? kTcRows : (S.n_scored + 7) / 8 * 8;      // (1024 bytes and more: boxes keep the swizzle's phase)
   cudaError_t e = cache_map(&mq, A.q, true, D, A.n_queries, A.total_rows / A.n_queries, box_rows);
   if (e == cudaSuccess) e = cache_map(&mk, A.K, true, D, A.cap, A.n_streams, kTcKeys);
+  if (e != cudaSuccess) return e;
+  // Up to two tiles of queries stay where they are, and the cached rows go by.
+  const int heads = A.n_rows / A.n_queries;
+  if (S.n_scored <= kTcRows && (heads + kTcRows / box_rows - 1) / (kTcRows / box_rows) <= 2) return launch_stream<D>(A, S, box_rows, mq, mk, st);
   static std::atomic<unsigned long long> devices{0};
-  if (e == cudaSuccess) e = kernel_limits(score_tc_kernel<D>, Shape<D>::kSmem, false, devices);
+  e = kernel_limits(score_tc_kernel<D>, Shape<D>::kSmem, false, devices);
   if (e != cudaSuccess) return e;
   // CTAs of a cluster: more while there are fewer than two waves and four tiles of queries are left for each.  (The CTAs of the first
   // rows, which all queries see, would otherwise still run when the others are done.)
