@@ -10,16 +10,15 @@
 
 namespace bkv {
 
-// A kernel's dynamic shared memory (and clusters of more than eight CTAs), set once per device: 0.4 us of every call otherwise.
+// A kernel's dynamic shared memory, set once per device: 0.4 us of every call otherwise.
 template <class Kern>
-cudaError_t kernel_limits(Kern kern, size_t smem, bool large_clusters, std::atomic<unsigned long long>& devices) {
+cudaError_t kernel_limits(Kern kern, size_t smem, std::atomic<unsigned long long>& devices) {
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   const unsigned long long bit = dev < 64 ? 1ull << dev : 0;
   if (devices.load(std::memory_order_acquire) & bit) return cudaSuccess;
   e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  if (e == cudaSuccess && large_clusters) e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   if (e == cudaSuccess) devices.fetch_or(bit, std::memory_order_release);
   return e;
 }

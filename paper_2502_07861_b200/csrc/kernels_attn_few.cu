@@ -620,7 +620,8 @@ __global__ void __launch_bounds__(kThreads, (Few<kBf16, D>::kCtas)) attn_few_ker
 // The splits of a stream as a cluster of CTAs, where its logits fit their shared memory: they join their sums through it, every
 // CTA then turns its own logits into weights, and nothing but results leaves the chip.  More than eight query rows are groups with a
 // cluster each; what a cached row receives from a group goes to `sums` [groups, n_streams, cap] (one group: to the scores).
-constexpr int kMaxCluster = 16;
+constexpr int kMaxCluster = 8;
+constexpr int most_clustered(int C) { return C > 4 ? 192 : 256; }       // CTAs of a launch, by clusters of C
 constexpr int logit_bytes(bool bf16, int d) { return !bf16 && d == 64 ? 8 * 1024 : 15 * 1024; }       // of a CTA: two (fp32, d = 128: one) still fit an SM
 
 template <bool kBf16, int D, int kR>
@@ -811,7 +812,7 @@ cudaError_t launch_few(const FewArgs& P, const FewArgs* also, bool finish, cudaS
   return for_rows<kBf16, D>(most, [&](auto rows) {
     auto kern = attn_few_kernel<kBf16, D, decltype(rows)::value>;
     static std::atomic<unsigned long long> devices{0};
-    const cudaError_t e = kernel_limits(kern, F::kSmem, false, devices);
+    const cudaError_t e = kernel_limits(kern, F::kSmem, devices);
     if (e != cudaSuccess) return e;
     const PdlConfig pc(dim3((unsigned)ctas), kThreads, F::kSmem, st);
     return cudaLaunchKernelEx(&pc.cfg, kern, J, maps);
@@ -831,7 +832,7 @@ cudaError_t launch_cluster(const AttnRows& A, const ScoreArgs& S, int C, float* 
   e = for_rows<kBf16, D>(A.n_rows, [&](auto rows) {
     auto kern = attn_few_cluster_kernel<kBf16, D, decltype(rows)::value>;
     static std::atomic<unsigned long long> devices{0};
-    const cudaError_t e = kernel_limits(kern, F::kSmem + logit_bytes(kBf16, D), true, devices);
+    const cudaError_t e = kernel_limits(kern, F::kSmem + logit_bytes(kBf16, D), devices);
     if (e != cudaSuccess) return e;
     const int pitch = logit_pitch(A.cap, C);
     PdlConfig pc(dim3(A.n_streams * groups, C), kThreads, F::kSmem + (size_t)std::min(A.n_rows, kFewRows) * pitch * 4, st);
@@ -867,13 +868,14 @@ int few_splits(int64_t streams, int cap, int n_rows) {
   return (int)std::max<int64_t>(1, std::min<int64_t>(std::max(fill, even), kAttnMaxSplits));
 }
 
-// CTAs of a stream's cluster, 0 where its logits do not fit or the clusters do not fit one wave: as many as leave a tile for every warp.
-// (256 streams of up to 8192 rows in clusters of 16 took 228 us, as splits of a launch 108: clusters start and end as a whole.)
+// CTAs of a stream's cluster, 0 where its logits do not fit or the launch would be too large: as many as leave a tile for every warp.  Clusters
+// start and end as a whole, so that they pay only while all of them run at once: 256 streams of up to 8192 rows in clusters of 16 took 228 us, as
+// splits of a launch 108; 32 x 1024 rows by clusters of 8 12.4 us, of 4 8.7; 16 x 2048 rows by clusters of 16 15.3, of 8 9.5.
 int few_cluster(int64_t streams, int cap, int n_rows, int d, int is_bf16) {
   const int64_t sets = streams * ((n_rows + kFewRows - 1) / kFewRows);
   int C = 1;
-  while (C < kMaxCluster && 2 * sets * C <= 2 * kAttnSms && cap > C * kWarps * kTile) C *= 2;
-  return sets * C <= 2 * kAttnSms && (int64_t)std::min(n_rows, kFewRows) * logit_pitch(cap, C) * 4 <= logit_bytes(is_bf16, d) ? C : 0;
+  while (C < kMaxCluster && 2 * sets * C <= most_clustered(2 * C) && cap > C * kWarps * kTile) C *= 2;
+  return sets * C <= most_clustered(C) && (int64_t)std::min(n_rows, kFewRows) * logit_pitch(cap, C) * 4 <= logit_bytes(is_bf16, d) ? C : 0;
 }
 // Floats of the workspace that they need.
 int64_t few_cluster_sums(const AttnRows& A) { return A.n_rows > kFewRows ? (int64_t)(A.n_rows + kFewRows - 1) / kFewRows * A.n_streams * A.cap : 0; }

@@ -234,7 +234,7 @@ __global__ void __launch_bounds__(kThreads) score_simt_kernel(const AttnRows A, 
 
 template <class Kern, class... Args>
 cudaError_t launch(Kern kern, std::atomic<unsigned long long>& devices, dim3 grid, size_t smem, cudaStream_t st, const Args&... args) {
-  const cudaError_t e = kernel_limits(kern, smem, false, devices);
+  const cudaError_t e = kernel_limits(kern, smem, devices);
   if (e != cudaSuccess) return e;
   const PdlConfig pc(grid, kThreads, smem, st);
   return cudaLaunchKernelEx(&pc.cfg, kern, args...);

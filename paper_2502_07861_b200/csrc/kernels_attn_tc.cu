@@ -418,7 +418,7 @@ cudaError_t launch(const TcArgs& P, cudaStream_t st) {
   if (e == cudaSuccess) e = cache_map(&mk, A.K, true, D, A.cap, A.n_streams, kTcKeys);
   if (e == cudaSuccess) e = cache_map(&mv, A.V, true, D, A.cap, A.n_streams, kTcKeys);
   static std::atomic<unsigned long long> devices{0};
-  if (e == cudaSuccess) e = kernel_limits(attn_tc_kernel<D, kWeighted>, Shape<D, kWeighted>::kSmem, false, devices);
+  if (e == cudaSuccess) e = kernel_limits(attn_tc_kernel<D, kWeighted>, Shape<D, kWeighted>::kSmem, devices);
   if (e != cudaSuccess) return e;
   const PdlConfig pc(dim3((unsigned)P.blocks * A.n_streams, A.splits), kThreads, Shape<D, kWeighted>::kSmem, st);
   return cudaLaunchKernelEx(&pc.cfg, attn_tc_kernel<D, kWeighted>, P, mq, mk, mv);

@@ -400,7 +400,7 @@ cudaError_t launch_evict(const EvictArgs& E, cudaStream_t st) {
   pc.cfg.numAttrs = 2;
   static std::atomic<unsigned long long> devices[2];
   auto kern = fused ? evict_select_kernel<true> : evict_select_kernel<false>;
-  cudaError_t e = kernel_limits(kern, kStageRows * 8, false, devices[fused]);
+  cudaError_t e = kernel_limits(kern, kStageRows * 8, devices[fused]);
   if (e == cudaSuccess) e = cudaLaunchKernelEx(&pc.cfg, kern, E, per, staged);
   if (e != cudaSuccess || fused || (E.in_place && E.list == 0)) return e;
   switch (E.row_bytes / 16) {

@@ -424,7 +424,7 @@ score_stream_kernel(const __grid_constant__ AttnRows A, const ScoreArgs C, int b
 template <int D>
 cudaError_t launch_stream(const AttnRows& A, const ScoreArgs& S, int box_rows, const CUtensorMap& mq, const CUtensorMap& mk, cudaStream_t st) {
   static std::atomic<unsigned long long> devices{0};
-  const cudaError_t e = kernel_limits(score_stream_kernel<D>, StreamShape<D>::kSmem, false, devices);
+  const cudaError_t e = kernel_limits(score_stream_kernel<D>, StreamShape<D>::kSmem, devices);
   if (e != cudaSuccess) return e;
   const int heads = A.n_rows / A.n_queries, pack = kTcRows / box_rows, q_tiles = (heads + pack - 1) / pack;
   const int cols = (std::min(heads, pack) * box_rows + 31) / 32 * 32;
@@ -446,7 +446,7 @@ cudaError_t launch(const AttnRows& A, const ScoreArgs& S, cudaStream_t st) {
   const int heads = A.n_rows / A.n_queries;
   if (S.n_scored <= kTcRows && (heads + kTcRows / box_rows - 1) / (kTcRows / box_rows) <= 2) return launch_stream<D>(A, S, box_rows, mq, mk, st);
   static std::atomic<unsigned long long> devices{0};
-  e = kernel_limits(score_tc_kernel<D>, Shape<D>::kSmem, false, devices);
+  e = kernel_limits(score_tc_kernel<D>, Shape<D>::kSmem, devices);
   if (e != cudaSuccess) return e;
   // CTAs of a cluster: more while there are fewer than two waves and four tiles of queries are left for each.  (The CTAs of the first
   // rows, which all queries see, would otherwise still run when the others are done.)
