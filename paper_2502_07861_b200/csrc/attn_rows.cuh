@@ -152,9 +152,10 @@ __device__ inline void join_splits(const AttnRows& A, int cta, JoinShared<D>& sh
   }
 }
 
-cudaError_t launch_attn_simt(const AttnRows& A, int d, int is_bf16, cudaStream_t st);
+int simt_row_tiles(int n_rows);
+cudaError_t launch_attn_simt(const AttnRows& A, int d, cudaStream_t st);      // fp32
 cudaError_t launch_attn_combine(const AttnRows& A, int d, int is_bf16, cudaStream_t st);
-cudaError_t launch_score_simt(const AttnRows& A, const ScoreArgs& S, int d, int is_bf16, cudaStream_t st);
+cudaError_t launch_score_simt(const AttnRows& A, const ScoreArgs& S, int d, cudaStream_t st);      // fp32
 
 int few_splits(int64_t streams, int cap, int n_rows);
 int64_t few_pitch(int cap);

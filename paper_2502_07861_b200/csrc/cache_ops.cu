@@ -35,9 +35,9 @@ int report(const char* what, cudaError_t e) {
   return e == cudaErrorMemoryAllocation ? BALANCEKV_E_NOMEM : BALANCEKV_E_CUDA;
 }
 
-// CTAs that share the keys of a tile of query rows: enough for two waves, but no fewer than two tiles of keys each.
+// CTAs that share the keys of a tile of query rows on CUDA cores: two waves of them at most, two tiles of keys each at least.
 int simt_splits(int64_t row_tiles, int cap) {
-  const int64_t key_tiles = (cap + 63) / 64, want = (2 * kAttnSms + row_tiles - 1) / row_tiles;
+  const int64_t key_tiles = (cap + 63) / 64, want = 2 * kAttnSms / row_tiles;
   return (int)std::max<int64_t>(1, std::min<int64_t>({want, key_tiles / 2, (int64_t)kAttnMaxSplits}));
 }
 
@@ -73,7 +73,7 @@ int plan_scored(AttnRows& A, float*& x, Pieces& ws, int n_streams, int capacity,
     x = ws.take<float>(few_cluster_sums(A));
     return BALANCEKV_OK;
   }
-  A.splits = few ? few_splits(n_streams, capacity, (int)rows) : dtype ? attn_tc_splits(A) : simt_splits((rows + 63) / 64 * n_streams, capacity);
+  A.splits = few ? few_splits(n_streams, capacity, (int)rows) : dtype ? attn_tc_splits(A) : simt_splits((int64_t)simt_row_tiles((int)rows) * n_streams, capacity);
   A.n_slots = !few && dtype ? attn_tc_slots(A, A.splits) : A.splits;
   take_parts(A, ws, head_dim);
   if (n_scored) A.lse = ws.take<float>(A.total_rows);
@@ -102,7 +102,7 @@ int plan_prefix(AttnRows& P, AttnRows& A, Pieces& ws, int prefix_len, int capaci
   P.q_stream = P.q_inner = group;
   P.q_outer = n_kv_heads * group;
   const bool few = prefix_by_few(P, dtype);
-  P.splits = few ? few_splits(n_kv_heads, prefix_len, P.n_rows) : dtype ? attn_tc_splits(P) : simt_splits((int64_t)(P.n_rows + 63) / 64 * n_kv_heads, prefix_len);
+  P.splits = few ? few_splits(n_kv_heads, prefix_len, P.n_rows) : dtype ? attn_tc_splits(P) : simt_splits((int64_t)simt_row_tiles(P.n_rows) * n_kv_heads, prefix_len);
   A.n_streams = (int)streams;                  // a sequence's own rows
   A.lens_div = n_kv_heads;
   A.cap = capacity;
@@ -174,9 +174,9 @@ extern "C" int balancekv_attn_scored(const void* K, const void* V, const int32_t
     if (e == cudaSuccess && n_scored) e = launch_few_end(A, x, S, head_dim, dtype, st);
     else if (e == cudaSuccess && A.n_slots > 1) e = launch_attn_combine(A, head_dim, dtype, st);
   } else {
-    e = dtype ? launch_attn_tc(A, head_dim, st) : launch_attn_simt(A, head_dim, dtype, st);
+    e = dtype ? launch_attn_tc(A, head_dim, st) : launch_attn_simt(A, head_dim, st);
     if (e == cudaSuccess && A.n_slots > 1) e = launch_attn_combine(A, head_dim, dtype, st);
-    if (e == cudaSuccess && n_scored) e = dtype ? launch_score_tc(A, S, head_dim, st) : launch_score_simt(A, S, head_dim, dtype, st);
+    if (e == cudaSuccess && n_scored) e = dtype ? launch_score_tc(A, S, head_dim, st) : launch_score_simt(A, S, head_dim, st);
   }
   return report("balancekv_attn_scored", e);
 }
@@ -218,7 +218,7 @@ extern "C" int balancekv_decode_attn_prefix(const void* K_prefix, const void* V_
   if (few) {
     e = launch_attn_few(P, nullptr, A.splits ? &A : nullptr, false, head_dim, dtype, st);
   } else {
-    e = dtype ? launch_attn_tc(P, head_dim, st) : launch_attn_simt(P, head_dim, dtype, st);
+    e = dtype ? launch_attn_tc(P, head_dim, st) : launch_attn_simt(P, head_dim, st);
     if (e == cudaSuccess && A.splits) e = launch_attn_few(A, nullptr, nullptr, finish, head_dim, dtype, st);
   }
   if (e == cudaSuccess && P.n_slots > 1 && !finish) e = launch_attn_combine(P, head_dim, dtype, st);
