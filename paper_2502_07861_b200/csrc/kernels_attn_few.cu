@@ -588,13 +588,16 @@ __global__ void __launch_bounds__(kThreads, (Few<kBf16, D>::kCtas)) attn_few_ker
   const int group = cta % J.groups[which], split = cta / J.groups[which] % A.splits, s = cta / J.groups[which] / A.splits;
   const Group G{group * kFewRows, min(kFewRows, A.n_rows - group * kFewRows)};
   few_init(sh, maps.k[which], maps.v[which]);
-  grid_wait_and_release();
+  // A launch that finishes the outputs follows the prefix's: until it joins their slots it reads nothing that writes, so that its CTAs start as
+  // the others leave.  (What came before the prefix's launch is complete: that releases its dependents behind its own wait.)
+  if (!J.finish) grid_wait_and_release();
   __syncthreads();
   const int len = attn_len(A, s), n_all = (len + kTile - 1) / kTile;
   const int64_t pitch = J.job[which].pitch;
   const Logits X{J.job[which].x ? J.job[which].x + ((int64_t)s * A.n_rows + G.r0) * pitch : nullptr, pitch};
   few_tiles(A, G, X, maps.k[which], maps.v[which], sh, tiles, s, len, (int)((int64_t)n_all * split / A.splits), (int)((int64_t)n_all * (split + 1) / A.splits));
   const float* mrg = reinterpret_cast<const float*>(tiles);
+  if (J.finish) grid_wait_and_release();
   for (int r = warp; r < G.g; r += kWarps) {
     float acc[D / 32], top, sum;
     few_join<D, kWarps>(kWarps, lane, [&](int w) { return mrg + (w * kFewRows + r) * F::kPitch; }, acc, top, sum);
@@ -722,20 +725,21 @@ __global__ void __launch_bounds__(kEndThreads, 6) few_end_kernel(const __grid_co
   __shared__ JoinShared<D> join;
   const AttnRows& A = P.A;
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
-  grid_wait_and_release();
   if ((int)blockIdx.x < joins) {
+    grid_wait_and_release();
     join_splits<kBf16, D, 2>(A, blockIdx.x, join);
     return;
   }
+  // What attn_few_kernel does not write is asked for before it has ended, and what does not depend on the sums ahead of them.
   const int s = ((int)blockIdx.x - joins) / chunks, k0 = ((int)blockIdx.x - joins) % chunks * kEndKeys;
   const int len = attn_len(A, s);
-  if (k0 >= len) return;
   constexpr int kPer = kEndKeys / kEndThreads;
-  // what does not depend on the sums is asked for first
   const float* x = P.x + (int64_t)s * A.n_rows * P.pitch + k0 + tid;
   float logit[kFewRows][kPer], old[kPer];
 #pragma unroll
   for (int j = 0; j < kPer; ++j) old[j] = k0 + tid + j * kEndThreads < len ? score_old(S, (int64_t)s * A.cap + k0 + tid + j * kEndThreads) : 0.f;
+  grid_wait_and_release();
+  if (k0 >= len) return;
 #pragma unroll
   for (int r = 0; r < kFewRows; ++r)
 #pragma unroll

@@ -84,7 +84,8 @@ score_tc_kernel(const __grid_constant__ AttnRows A, const ScoreArgs C, int box_r
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_s)), "r"(256u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  grid_wait_and_release();
+  // (Only the loading warp waits for the attention kernel to end, before it reads its lse: nothing else here is written by it, and what came
+  // before it is complete.)
   // the first cached rows, which the most queries see, first
   const int s = blockIdx.x % A.n_streams, key0 = blockIdx.x / A.n_streams * kTcKeys;
   const int len = attn_len(A, s), m = A.n_queries, heads = A.n_rows / m;
@@ -110,6 +111,7 @@ score_tc_kernel(const __grid_constant__ AttnRows A, const ScoreArgs C, int box_r
 
   if (warp >= 8) {
     regs_down<kRegsOther>();
+    if (warp == 8 && n == 0) grid_wait_and_release();
     if (warp == 8 && n > 0) {
       bool ok = true;
       if (lane == 0) {
@@ -137,6 +139,7 @@ score_tc_kernel(const __grid_constant__ AttnRows A, const ScoreArgs C, int box_r
             for (int b = 0; b < D / 64; ++b)
               tma_load_3d(ring + slot * Sh::kTile + b * Sh::kBox + h * box_rows * 128, &mq, 64 * b, j, s * heads + head + h, q_full + slot);
         }
+        if (i == 0) grid_wait_and_release();
         // rows behind a head's last are zeros, of weight zero
 #pragma unroll
         for (int c = 0; c < kTcRows / 32; ++c) {
@@ -294,10 +297,23 @@ score_stream_kernel(const __grid_constant__ AttnRows A, const ScoreArgs C, int b
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_s)), "r"(512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  grid_wait_and_release();
   const int s = blockIdx.x, len = attn_len(A, s), m = A.n_queries, heads = A.n_rows / m, start = m - C.n_scored;
   const int all = (len + kTcKeys - 1) / kTcKeys;
   const int t0 = (int)((int64_t)all * blockIdx.y / gridDim.y), n = (int)((int64_t)all * (blockIdx.y + 1) / gridDim.y) - t0;      // this CTA's
+  // The queries and the first cached rows come in before the attention kernel has ended, whose lse alone is waited for.
+  auto ask_keys = [&](int i) {
+    mbar_expect_tx(k_full + i % kRing, Sh::kTile);
+    for (int b = 0; b < D / 64; ++b) tma_load_3d(ring + i % kRing * Sh::kTile + b * Sh::kBox, &mk, 64 * b, (t0 + i) * kTcKeys, s, k_full + i % kRing);
+  };
+  __syncthreads();
+  if (tid == 8 * 32 && n > 0) {
+    mbar_expect_tx(&q_full, (uint32_t)heads * box_rows * 2 * D);
+    for (int h = 0; h < heads; ++h)
+      for (int b = 0; b < D / 64; ++b)
+        tma_load_3d(sm + h / pack * Sh::kTile + b * Sh::kBox + h % pack * box_rows * 128, &mq, 64 * b, start, s * heads + h, &q_full);
+    for (int i = 0; i < min(kRing, n); ++i) ask_keys(i);
+  }
+  grid_wait_and_release();
   // query row r of tile t: head and query (box_rows = 128: a head to a tile)
   if (n > 0)
     for (int i = tid; i < 2 * kTcRows; i += kThreads) {
@@ -312,21 +328,11 @@ score_stream_kernel(const __grid_constant__ AttnRows A, const ScoreArgs C, int b
 
   if (warp == 8 && n > 0) {
     bool ok = true;
-    if (lane == 0) {
-      mbar_expect_tx(&q_full, (uint32_t)heads * box_rows * 2 * D);
-      for (int h = 0; h < heads; ++h)
-        for (int b = 0; b < D / 64; ++b)
-          tma_load_3d(sm + h / pack * Sh::kTile + b * Sh::kBox + h % pack * box_rows * 128, &mq, 64 * b, start, s * heads + h, &q_full);
-    }
-    int i = 0;
+    int i = min(kRing, n);
     for (; i < n; ++i) {
-      const int slot = i % kRing;
-      if (i >= kRing) ok = wait_bar(k_empty + slot, (uint32_t)(i / kRing - 1) & 1u, &abort_flag);
+      ok = wait_bar(k_empty + i % kRing, (uint32_t)(i / kRing - 1) & 1u, &abort_flag);
       if (!__all_sync(0xffffffffu, ok)) break;
-      if (lane == 0) {
-        mbar_expect_tx(k_full + slot, Sh::kTile);
-        for (int b = 0; b < D / 64; ++b) tma_load_3d(ring + slot * Sh::kTile + b * Sh::kBox, &mk, 64 * b, (t0 + i) * kTcKeys, s, k_full + slot);
-      }
+      if (lane == 0) ask_keys(i);
       __syncwarp();
     }
     if (i < n && lane == 0) {                    // gave up: the copies in flight, within limits
