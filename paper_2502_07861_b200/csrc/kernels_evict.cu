@@ -34,7 +34,7 @@ __device__ inline uint32_t score_key(float x) {
 
 struct SelectShared {
   __align__(16) uint32_t hist[kPasses][kBins];
-  uint32_t coarse[kPasses][kBins / 64];          // sums of 64 bins
+  uint32_t coarse[kPasses][kMaxCluster][kBins / 64];          // every CTA's sums of 64 bins
   int warp_a[kWarps], warp_b[kWarps];
   int cta[3][2];                                 // what the cluster's CTAs tell one another, a place per exchange
   int before_a, before_b, all_a;                 // of the CTAs before this one; of all
@@ -253,7 +253,8 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const EvictArgs 
       uint32_t n = h.x + h.y + h.z + h.w;
 #pragma unroll
       for (int o = 8; o > 0; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
-      if (tid % 16 == 0) sh.coarse[pass][tid / 16] = n;
+      // to every CTA of the cluster (a store does not wait, a load from there does)
+      if (tid % 16 < C) cluster.map_shared_rank(&sh.coarse[pass][c][0], tid % 16)[tid / 16] = n;
     }
     cluster.sync();
     // One warp finds the digit, from the largest down: which 64 bins, then which of them.  (Every thread adding the cluster's bins up
@@ -262,16 +263,17 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const EvictArgs 
       int n = 0, before, rest;
 #pragma unroll
       for (int b = 0; b < kMaxCluster; ++b)
-        if (b < C) n += (int)cluster.map_shared_rank(&sh.coarse[pass][0], b)[31 - lane];
+        if (b < C) n += (int)sh.coarse[pass][b][31 - lane];
       const int group = 31 - lane_of(n, need, before);
-      int hi = 0, lo = 0;                        // the bins 63 - 2 lane, 62 - 2 lane of the 64
+      int hi = 0, lo = 0;                        // the bins 63 - 2 lane, 62 - 2 lane of the 64; all CTAs' asked for at once
+      uint2 h[kMaxCluster];
 #pragma unroll
-      for (int b = 0; b < kMaxCluster; ++b)
-        if (b < C) {
-          const uint2 h = *reinterpret_cast<const uint2*>(cluster.map_shared_rank(&sh.hist[pass][0], b) + 64 * group + 62 - 2 * lane);
-          hi += (int)h.y;
-          lo += (int)h.x;
-        }
+      for (int b = 0; b < kMaxCluster; ++b) h[b] = *reinterpret_cast<const uint2*>(cluster.map_shared_rank(&sh.hist[pass][0], min(b, C - 1)) + 64 * group + 62 - 2 * lane);
+#pragma unroll
+      for (int b = 0; b < kMaxCluster; ++b) {
+        hi += b < C ? (int)h[b].y : 0;
+        lo += b < C ? (int)h[b].x : 0;
+      }
       const int at = lane_of(hi + lo, need - before, rest);
       const int first_hi = __shfl_sync(0xffffffffu, hi, at);
       const bool low = need - before - rest > first_hi;
@@ -285,23 +287,40 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const EvictArgs 
     need -= sh.above;
   }
 
-  // A warp takes neighbouring rows, so that ranks follow from ballots.
+  // A warp takes neighbouring rows, so that ranks follow from ballots; four times 32 at once.
+  constexpr int kUnroll = 4;
   const int seg = (per + kWarps - 1) / kWarps, w0 = min(end, begin + warp * seg), w1 = min(end, w0 + seg);
   const uint32_t lower = (1u << lane) - 1u;
   int eq_before = 0, none = 0, all = 0;
-  for (int i = w0; i < w1; i += 32) eq_before += __popc(__ballot_sync(0xffffffffu, i + lane < w1 && key(i + lane) == prefix));
+  for (int i = w0; i < w1; i += 32 * kUnroll) {
+    uint32_t u[kUnroll];
+#pragma unroll
+    for (int j = 0; j < kUnroll; ++j) u[j] = i + 32 * j + lane < w1 ? key(i + 32 * j + lane) : ~prefix;
+#pragma unroll
+    for (int j = 0; j < kUnroll; ++j) eq_before += __popc(__ballot_sync(0xffffffffu, u[j] == prefix));
+  }
   sums_before(cluster, sh, 1, C, c, eq_before, none, all);
   // every row of the warp's: whether it is a hole or moves
   auto walk = [&](auto&& each) {
     int equal = eq_before;
-    for (int i = w0; i < w1; i += 32) {
-      const int row = i + lane;
-      const bool held = row < w1;
-      const uint32_t u = held ? key(row) : 0u;
-      const uint32_t same = __ballot_sync(0xffffffffu, held && u == prefix);
-      const bool kept = held && (u > prefix || (u == prefix && equal + __popc(same & lower) < need));
-      equal += __popc(same);
-      each(row, __ballot_sync(0xffffffffu, held && !kept && row < k), __ballot_sync(0xffffffffu, kept && row >= k), kept);
+    for (int i = w0; i < w1; i += 32 * kUnroll) {
+      uint32_t u[kUnroll], same[kUnroll], hole[kUnroll], mover[kUnroll];
+      bool kept[kUnroll];
+#pragma unroll
+      for (int j = 0; j < kUnroll; ++j) u[j] = i + 32 * j + lane < w1 ? key(i + 32 * j + lane) : 0u;
+#pragma unroll
+      for (int j = 0; j < kUnroll; ++j) same[j] = __ballot_sync(0xffffffffu, i + 32 * j + lane < w1 && u[j] == prefix);
+#pragma unroll
+      for (int j = 0; j < kUnroll; ++j) {
+        const int row = i + 32 * j + lane;
+        const bool held = row < w1;
+        kept[j] = held && (u[j] > prefix || (u[j] == prefix && equal + __popc(same[j] & lower) < need));
+        equal += __popc(same[j]);
+        hole[j] = __ballot_sync(0xffffffffu, held && !kept[j] && row < k);
+        mover[j] = __ballot_sync(0xffffffffu, kept[j] && row >= k);
+      }
+#pragma unroll
+      for (int j = 0; j < kUnroll; ++j) each(i + 32 * j + lane, hole[j], mover[j], kept[j]);
     }
   };
   int at_hole = 0, at_mover = 0;
