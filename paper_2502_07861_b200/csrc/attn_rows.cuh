@@ -123,6 +123,7 @@ __device__ inline void join_splits(const AttnRows& A, int cta, JoinShared<D>& sh
         for (int j = 0; j < kAhead; ++j) {
           const float w = __shfl_sync(0xffffffffu, f[k], i0 + j * ways & 31);
           if (i0 + j * ways >= min(32 * k + 32, A.n_slots)) break;
+          if (w == 0.f) continue;                // an empty slot, whose sums are not written
 #pragma unroll
           for (int c = 0; c < kPer; ++c) acc[c] = fmaf(v[j][c], w, acc[c]);
         }
@@ -157,7 +158,7 @@ cudaError_t launch_attn_simt(const AttnRows& A, int d, cudaStream_t st);      //
 cudaError_t launch_attn_combine(const AttnRows& A, int d, int is_bf16, cudaStream_t st);
 cudaError_t launch_score_simt(const AttnRows& A, const ScoreArgs& S, int d, cudaStream_t st);      // fp32
 
-int few_splits(int64_t streams, int cap, int n_rows);
+int few_splits(int64_t streams, int cap, int n_rows, int d, int is_bf16);
 int64_t few_pitch(int cap);
 cudaError_t launch_attn_few(const AttnRows& A, float* x, const AttnRows* also, bool finish, int d, int is_bf16, cudaStream_t st);
 int few_cluster(int64_t streams, int cap, int n_rows, int d, int is_bf16);

@@ -73,7 +73,7 @@ int plan_scored(AttnRows& A, float*& x, Pieces& ws, int n_streams, int capacity,
     x = ws.take<float>(few_cluster_sums(A));
     return BALANCEKV_OK;
   }
-  A.splits = few ? few_splits(n_streams, capacity, (int)rows) : dtype ? attn_tc_splits(A) : simt_splits((int64_t)simt_row_tiles((int)rows) * n_streams, capacity);
+  A.splits = few ? few_splits(n_streams, capacity, (int)rows, head_dim, dtype) : dtype ? attn_tc_splits(A) : simt_splits((int64_t)simt_row_tiles((int)rows) * n_streams, capacity);
   A.n_slots = !few && dtype ? attn_tc_slots(A, A.splits) : A.splits;
   take_parts(A, ws, head_dim);
   if (n_scored) A.lse = ws.take<float>(A.total_rows);
@@ -102,12 +102,12 @@ int plan_prefix(AttnRows& P, AttnRows& A, Pieces& ws, int prefix_len, int capaci
   P.q_stream = P.q_inner = group;
   P.q_outer = n_kv_heads * group;
   const bool few = prefix_by_few(P, dtype);
-  P.splits = few ? few_splits(n_kv_heads, prefix_len, P.n_rows) : dtype ? attn_tc_splits(P) : simt_splits((int64_t)simt_row_tiles(P.n_rows) * n_kv_heads, prefix_len);
+  P.splits = few ? few_splits(n_kv_heads, prefix_len, P.n_rows, head_dim, dtype) : dtype ? attn_tc_splits(P) : simt_splits((int64_t)simt_row_tiles(P.n_rows) * n_kv_heads, prefix_len);
   A.n_streams = (int)streams;                  // a sequence's own rows
   A.lens_div = n_kv_heads;
   A.cap = capacity;
   A.n_rows = A.q_stream = A.q_inner = group;
-  A.splits = capacity ? few_splits(streams, capacity, group) : 0;
+  A.splits = capacity ? few_splits(streams, capacity, group, head_dim, dtype) : 0;
   A.slot0 = !few && dtype ? attn_tc_slots(P, P.splits) : P.splits;
   P.n_slots = A.n_slots = A.slot0 + A.splits;
   take_parts(P, ws, head_dim);

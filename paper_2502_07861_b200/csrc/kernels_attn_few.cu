@@ -31,6 +31,10 @@ constexpr int kTile = 32;                        // rows
 constexpr float kGrow = 8.f;                     // a maximum follows when it would grow by more: weights stay below 2^8
 constexpr uint32_t kBox = kTile * 128;           // bytes
 
+// Query rows of a CTA: eight, of fp32 rows with 128 dims four, whose sums and queries fit the registers (eight query rows over 8 x 16384 such
+// rows: 63.8 us by eight, FOUR by four, which read the rows twice, the second time from L2).
+__host__ __device__ constexpr int group_rows(bool bf16, int d) { return !bf16 && d == 128 ? 4 : kFewRows; }
+
 template <bool kBf16, int D>
 struct Few {
   static constexpr int kEsz = kBf16 ? 2 : 4, kBoxDims = 128 / kEsz, kBoxes = D / kBoxDims;
@@ -50,7 +54,8 @@ struct FewArgs {
 // What a launch does: one set of streams, or two (a shared prefix and the sequences' own rows).
 struct FewJobs {
   FewArgs job[2];
-  int32_t groups[2];      // of eight query rows
+  int32_t groups[2];      // of query rows
+  int32_t least[2];       // tiles of a CTA, where the stream has them: of shorter streams the last splits are left empty
   int32_t ctas0;          // CTAs of the first set
   int32_t finish;         // one set of one split: the slots before its own are complete, and it joins them itself
 };
@@ -586,16 +591,22 @@ __global__ void __launch_bounds__(kThreads, (Few<kBf16, D>::kCtas)) attn_few_ker
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   // the groups of a stream's query rows next to one another: they read the same rows
   const int group = cta % J.groups[which], split = cta / J.groups[which] % A.splits, s = cta / J.groups[which] / A.splits;
-  const Group G{group * kFewRows, min(kFewRows, A.n_rows - group * kFewRows)};
+  constexpr int kGroup = group_rows(kBf16, D);
+  const Group G{group * kGroup, min(kGroup, A.n_rows - group * kGroup)};
   few_init(sh, maps.k[which], maps.v[which]);
   // A launch that finishes the outputs follows the prefix's: until it joins their slots it reads nothing that writes, so that its CTAs start as
   // the others leave.  (What came before the prefix's launch is complete: that releases its dependents behind its own wait.)
   if (!J.finish) grid_wait_and_release();
   __syncthreads();
   const int len = attn_len(A, s), n_all = (len + kTile - 1) / kTile;
+  const int used = max(1, min(A.splits, (n_all + J.least[which] - 1) / J.least[which]));      // splits
+  if (split >= used) {
+    if (warp == 0 && lane < G.g) A.part_ml[(int64_t)(A.slot0 + split) * A.total_rows + attn_row(A, s, G.r0 + lane)] = make_float2(-INFINITY, 0.f);
+    return;
+  }
   const int64_t pitch = J.job[which].pitch;
   const Logits X{J.job[which].x ? J.job[which].x + ((int64_t)s * A.n_rows + G.r0) * pitch : nullptr, pitch};
-  few_tiles(A, G, X, maps.k[which], maps.v[which], sh, tiles, s, len, (int)((int64_t)n_all * split / A.splits), (int)((int64_t)n_all * (split + 1) / A.splits));
+  few_tiles(A, G, X, maps.k[which], maps.v[which], sh, tiles, s, len, (int)((int64_t)n_all * split / used), (int)((int64_t)n_all * (split + 1) / used));
   const float* mrg = reinterpret_cast<const float*>(tiles);
   if (J.finish) grid_wait_and_release();
   for (int r = warp; r < G.g; r += kWarps) {
@@ -783,10 +794,11 @@ __global__ void __launch_bounds__(kEndThreads, 6) few_end_kernel(const __grid_co
   }
 }
 
-// kR for the call's rows.
-template <bool kBf16, int D, class Run>
+// kR for n_rows query rows, of which a CTA takes kMost at most.
+template <bool kBf16, int kMost, class Run>
 cudaError_t for_rows(int n_rows, Run run) {
   if constexpr (kBf16) return run(std::integral_constant<int, 8>{});
+  else if constexpr (kMost == 4) return n_rows <= 2 ? run(std::integral_constant<int, 2>{}) : run(std::integral_constant<int, 4>{});
   else return n_rows <= 2 ? run(std::integral_constant<int, 2>{}) : n_rows <= 4 ? run(std::integral_constant<int, 4>{}) : run(std::integral_constant<int, 8>{});
 }
 
@@ -803,8 +815,10 @@ cudaError_t launch_few(const FewArgs& P, const FewArgs* also, bool finish, cudaS
     cudaError_t e = cache_map(&maps.k[i], A.K, kBf16, D, A.cap, A.n_streams, kTile);
     if (e == cudaSuccess) e = cache_map(&maps.v[i], A.V, kBf16, D, A.cap, A.n_streams, kTile);
     if (e != cudaSuccess) return e;
-    J.groups[i] = (A.n_rows + kFewRows - 1) / kFewRows;
-    ctas += (int64_t)J.groups[i] * A.splits * A.n_streams;
+    J.groups[i] = (A.n_rows + group_rows(kBf16, D) - 1) / group_rows(kBf16, D);
+    const int64_t mine = (int64_t)J.groups[i] * A.splits * A.n_streams;
+    J.least[i] = kWarps * (mine > 4 * kAttnSms ? 8 : 1);
+    ctas += mine;
     if (i == 0) J.ctas0 = (int)ctas;
     most = std::max(most, A.n_rows);
   }
@@ -813,7 +827,7 @@ cudaError_t launch_few(const FewArgs& P, const FewArgs* also, bool finish, cudaS
     maps.v[1] = maps.v[0];
   }
   if (ctas > INT32_MAX) return cudaErrorInvalidValue;
-  return for_rows<kBf16, D>(most, [&](auto rows) {
+  return for_rows<kBf16, group_rows(kBf16, D)>(most, [&](auto rows) {
     auto kern = attn_few_kernel<kBf16, D, decltype(rows)::value>;
     static std::atomic<unsigned long long> devices{0};
     const cudaError_t e = kernel_limits(kern, F::kSmem, devices);
@@ -833,7 +847,7 @@ cudaError_t launch_cluster(const AttnRows& A, const ScoreArgs& S, int C, float* 
   if (e == cudaSuccess) e = cache_map(&mv, A.V, kBf16, D, A.cap, A.n_streams, kTile);
   if (e != cudaSuccess) return e;
   const int groups = (A.n_rows + kFewRows - 1) / kFewRows;
-  e = for_rows<kBf16, D>(A.n_rows, [&](auto rows) {
+  e = for_rows<kBf16, kFewRows>(A.n_rows, [&](auto rows) {
     auto kern = attn_few_cluster_kernel<kBf16, D, decltype(rows)::value>;
     static std::atomic<unsigned long long> devices{0};
     const cudaError_t e = kernel_limits(kern, F::kSmem + logit_bytes(kBf16, D), devices);
@@ -865,8 +879,8 @@ cudaError_t launch_end(const FewArgs& P, const ScoreArgs& S, cudaStream_t st) {
 
 // Split factor of the kernels above: as many CTAs as fit the SMs at once, with a tile for each warp; and of long caches, in parts of 1024
 // rows, up to six times as many, so that streams of different lengths even out (256 streams of up to 8192 rows: 104.9 us by 5 splits, 102.2 by 7).
-int few_splits(int64_t streams, int cap, int n_rows) {
-  const int64_t sets = streams * ((n_rows + kFewRows - 1) / kFewRows);
+int few_splits(int64_t streams, int cap, int n_rows, int d, int is_bf16) {
+  const int64_t sets = streams * ((n_rows + group_rows(is_bf16, d) - 1) / group_rows(is_bf16, d));
   const int64_t fill = std::min<int64_t>(2 * kAttnSms / sets, (cap + kWarps * kTile - 1) / (kWarps * kTile));
   const int64_t even = std::min<int64_t>((12 * kAttnSms + sets - 1) / sets, cap / 1024);
   return (int)std::max<int64_t>(1, std::min<int64_t>(std::max(fill, even), kAttnMaxSplits));
