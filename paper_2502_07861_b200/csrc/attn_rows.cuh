@@ -59,6 +59,21 @@ __device__ inline int attn_limit(const AttnRows& A, int len, int r) {
   return max(0, min(len, len - A.n_queries + r % A.n_queries + 1));
 }
 
+// The sums over `kG` neighbouring lanes of a[0], .., a[kG - 1], that of a[i] to the lane i of them: kG - 1 exchanges.
+template <int kG>
+__device__ inline float sum_scatter(float (&a)[kG], int lane) {
+#pragma unroll
+  for (int off = kG / 2; off > 0; off /= 2) {
+    const bool upper = lane & off;
+#pragma unroll
+    for (int i = 0; i < off; ++i) {
+      const float give = upper ? a[i] : a[i + off], keep = upper ? a[i + off] : a[i];
+      a[i] = keep + __shfl_xor_sync(0xffffffffu, give, off);
+    }
+  }
+  return a[0];
+}
+
 // The sums of what every row received: score_out = decay score_in + sum over heads and the newest n_scored queries of 2^(x - lse).
 struct ScoreArgs {
   const float* in;          // [n_streams, cap]; null: zeros
