@@ -32,7 +32,7 @@ constexpr float kGrow = 8.f;                     // a maximum follows when it wo
 constexpr uint32_t kBox = kTile * 128;           // bytes
 
 // Query rows of a CTA: eight, of fp32 rows with 128 dims four, whose sums and queries fit the registers (eight query rows over 8 x 16384 such
-// rows: 63.8 us by eight, FOUR by four, which read the rows twice, the second time from L2).
+// rows: 63.8 us by eight, 46.4 by four, which read the rows twice, the second time from L2).
 __host__ __device__ constexpr int group_rows(bool bf16, int d) { return !bf16 && d == 128 ? 4 : kFewRows; }
 
 template <bool kBf16, int D>
@@ -280,21 +280,6 @@ __device__ inline void few_warp_bf16(const AttnRows& A, const Group& G, const Lo
     for (int n = 0; n < kMB; ++n) { to[16 * n + hq] = o[n][e]; to[16 * n + 8 + hq] = o[n][2 + e]; }
     if (hq == 0) { to[D] = m[e]; to[D + 1] = l[e]; }
   }
-}
-
-// The sums over `kG` neighbouring lanes of a[0], .., a[kG - 1], that of a[i] to the lane i of them: kG - 1 exchanges.
-template <int kG>
-__device__ inline float sum_scatter(float (&a)[kG], int lane) {
-#pragma unroll
-  for (int off = kG / 2; off > 0; off /= 2) {
-    const bool upper = lane & off;
-#pragma unroll
-    for (int i = 0; i < off; ++i) {
-      const float give = upper ? a[i] : a[i + off], keep = upper ? a[i + off] : a[i];
-      a[i] = keep + __shfl_xor_sync(0xffffffffu, give, off);
-    }
-  }
-  return a[0];
 }
 
 // The same with FFMA; kR >= g rows.  What bounds it is shared memory, whose loads return 128 bytes a cycle whether lanes read the same or not, so
@@ -886,14 +871,17 @@ int few_splits(int64_t streams, int cap, int n_rows, int d, int is_bf16) {
   return (int)std::max<int64_t>(1, std::min<int64_t>(std::max(fill, even), kAttnMaxSplits));
 }
 
-// CTAs of a stream's cluster, 0 where its logits do not fit or the launch would be too large: as many as leave a tile for every warp.  Clusters
-// start and end as a whole, so that they pay only while all of them run at once: 256 streams of up to 8192 rows in clusters of 16 took 228 us, as
-// splits of a launch 108; 32 x 1024 rows by clusters of 8 12.4 us, of 4 8.7; 16 x 2048 rows by clusters of 16 15.3, of 8 9.5.
+// CTAs of a stream's cluster, 0 where clusters do not serve the call: as many as leave a tile for every warp.  What they save is the second
+// launch and the workspace, 4.4 us of the host's time (8 x 1024 rows: 11.1 us a call against 15.5; in a graph 7.1 against 7.3), and what they
+// cost are their meetings, so that they serve small calls: the logits fit shared memory, a CTA reads 256 KB at most (4 x 5000 fp32 rows of 128
+// dims, 640 KB each: 26.7 us against 20.7), and all clusters run at once, since they start and end as a whole (256 streams of up to 8192
+// rows in clusters of 16: 228 us against 108; 32 x 1024 rows by clusters of 8 12.4 us, of 4 8.7).
 int few_cluster(int64_t streams, int cap, int n_rows, int d, int is_bf16) {
   const int64_t sets = streams * ((n_rows + kFewRows - 1) / kFewRows);
   int C = 1;
   while (C < kMaxCluster && 2 * sets * C <= most_clustered(2 * C) && cap > C * kWarps * kTile) C *= 2;
-  return sets * C <= most_clustered(C) && (int64_t)std::min(n_rows, kFewRows) * logit_pitch(cap, C) * 4 <= logit_bytes(is_bf16, d) ? C : 0;
+  const int64_t rows = logit_pitch(cap, C);
+  return sets * C <= most_clustered(C) && std::min(n_rows, kFewRows) * rows * 4 <= logit_bytes(is_bf16, d) && rows * 2 * d * (is_bf16 ? 2 : 4) <= 256 << 10 ? C : 0;
 }
 // Floats of the workspace that they need.
 int64_t few_cluster_sums(const AttnRows& A) { return A.n_rows > kFewRows ? (int64_t)(A.n_rows + kFewRows - 1) / kFewRows * A.n_streams * A.cap : 0; }

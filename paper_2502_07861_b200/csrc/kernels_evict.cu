@@ -124,7 +124,7 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const EvictArgs 
   grid_wait_and_release();
   const int len = E.lens ? max(0, min(E.lens[s], E.cap)) : E.cap, k = min(len, E.keep);
   const int64_t first = (int64_t)s * E.cap;
-  int* holes = E.moves + (int64_t)s * (2 * E.list + (E.in_place ? 0 : E.keep));
+  int* holes = E.moves + (int64_t)s * (2 * (int64_t)E.list + (E.in_place ? 0 : E.keep));
   int* movers = holes + E.list;
   int* source = movers + E.list;
   if (len <= E.keep) {                           // nothing to evict (the same for the whole cluster, which has read lens by its barrier)
@@ -357,7 +357,7 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const EvictArg
   const int s = blockIdx.x / blocks, lane = threadIdx.x % kVecs;
   const int i0 = blockIdx.x % blocks * kGroups * kMoveRows + threadIdx.x / kVecs;
   grid_wait_and_release();
-  const int* holes = E.moves + (int64_t)s * (2 * E.list + (E.in_place ? 0 : E.keep));
+  const int* holes = E.moves + (int64_t)s * (2 * (int64_t)E.list + (E.in_place ? 0 : E.keep));
   const int* source = holes + (E.in_place ? E.list : 2 * E.list);
   const int n = E.in_place ? E.n_moves[s] : E.lens_out ? E.lens_out[s] : min(E.lens ? max(0, min(E.lens[s], E.cap)) : E.cap, E.keep);
   int64_t from[kMoveRows], to[kMoveRows];
@@ -403,7 +403,9 @@ cudaError_t launch_evict(const EvictArgs& E, cudaStream_t st) {
   while (C < kMaxCluster && E.cap > 2048 * C) C *= 2;
   // One launch where every CTA has an SM to itself and little to copy; larger clusters share the copying.  The second launch costs the
   // host 2.5 us and the device 4; a CTA moves about 100 KB a microsecond, half of that where sources come from a list (1 stream, 4000 of 16000
-  // rows by 8 CTAs with 512 KB each: 26 us against 17 by two launches; 64 streams, 1024 of 1025: 15.6 us a call against 18.2).
+  // rows by 8 CTAs with 512 KB each: 26 us against 17 by two launches; 64 streams, 1024 of 1025: 15.6 us a call against 18.2).  With more
+  // CTAs than SMs the copying waits in each CTA's turn, however little it is (1000 streams, one row of 1025 moved in place: 31.4 us
+  // by one launch, 17.0 by two, a copy of lens included).
   const int64_t bytes = 4 * (int64_t)E.row_bytes * (E.in_place ? E.list : std::min(E.keep, E.cap));
   int F = C;
   while (F < kMaxCluster && 2 * F * E.n_streams <= kAttnSms && bytes > F * ((int64_t)128 << 10)) F *= 2;
