@@ -205,7 +205,8 @@ int balancekv_decode_attn_static_status(int* status_host, void* stream);
  * use) holds the rows in use, of which a call attends no more than the capacity.  Rows behind the last may hold anything;
  * the rows in use are finite.  Each call works in a workspace of the caller (device, 256-byte aligned, at least the bytes that the
  * _workspace call of the same arguments gives on the host; contents need not be kept or cleared).  Calls that may overlap, graph replays
- * among them, need workspaces of their own.  Nothing is allocated and nothing synchronised; every call may be captured.  Memory that a
+ * among them, need workspaces of their own.  Nothing is allocated and nothing synchronised; every call may be captured.
+ * Device-side waits are bounded; should one give up, the floating-point results of its launch are NaN.  Memory that a
  * call writes overlaps nothing else that it is given, unless stated.  Errors: BALANCEKV_E_INVAL for bad arguments,
  * BALANCEKV_E_NOMEM for too small a workspace, BALANCEKV_E_CUDA. */
 
@@ -244,7 +245,7 @@ int balancekv_cache_evict_workspace(int n_streams, int capacity, int n_keep, int
  *       / (sum_{prefix} w_i e^{<k_i,q>/sqrt d}     + sum_{own rows} e^{<k_i,q>/sqrt d}),
  * Theorem 3.3's estimator where the prefix is a compressed stream (rows and weights as balancekv_cache_view gives them).
  * K_prefix, V_prefix: [n_kv_heads, prefix_len, head_dim], prefix_len >= 1; w_prefix (may be NULL: ones): float32 [n_kv_heads,
- * prefix_len], >= 0; a row of weight 0 counts as absent whatever it holds.  K, V: [n_seqs, n_kv_heads, capacity, head_dim], capacity >= 0
+ * prefix_len], finite and >= 0; a row of weight 0 counts as absent whatever it holds.  K, V: [n_seqs, n_kv_heads, capacity, head_dim], capacity >= 0
  * (0: no own rows, K and V may be NULL); lens: [n_seqs].  q, out: [n_seqs, n_kv_heads * group, head_dim]. */
 int balancekv_decode_attn_prefix(const void* K_prefix, const void* V_prefix, const float* w_prefix, int prefix_len, const void* K,
                                  const void* V, const int32_t* lens, int capacity, const void* q, void* out, int n_seqs,

@@ -78,6 +78,44 @@ def test_many_queries(cuda_lib, dtype, d, g, cap, lens, m, n_scored):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("d,g,cap,lens,m,n_scored", [
+    (128, 2, 60, [60, 4, 3, 1, 0], 4, 2), (64, 2, 40000, [40000, 39999, 2], 4, 3), (128, 1, 9000, [9000, 8999, 7, 8], 8, 8), (64, 4, 30000, [29999], 2, 1),
+    (128, 2, 3000, [(61 * s) % 3001 for s in range(300)], 3, 1), (128, 3, 12000, [12000, 100, 11999], 2, 2),
+])
+def test_a_handful_of_queries(cuda_lib, dtype, d, g, cap, lens, m, n_scored):
+    """Up to eight query rows, drafted tokens' say: the one-pass kernels, every query with a limit of its own."""
+    _check_scored(cuda_lib, dtype, d, g, cap, lens, m, n_scored, seed=cap)
+
+
+@pytest.mark.parametrize("dtype,cap", [("bf16", 6300000), ("fp32", 3200000)])
+def test_offsets_beyond_32_bits(cuda_lib, dtype, cap):
+    """The last stream of caches of more than 2^32 bytes, by the one-pass kernels, the tiles and the eviction."""
+    t, lens, d = TYPES[dtype], [5, 0, 700], 128
+    k, v = torch.zeros(3, cap, d, dtype=t, device="cuda"), torch.zeros(3, cap, d, dtype=t, device="cuda")
+    for s, n in enumerate(lens):
+        if n:
+            k[s, :n], v[s, :n] = _keys(20 + s, n, d, dtype=t), _normal(30 + s, n, d, dtype=t)
+        k[s, n:n + 300] = math.nan
+        v[s, n:n + 300] = math.nan
+    for m, g in ((1, 4), (20, 2)):
+        q = _normal(m, 3, g, m, d, dtype=t)
+        out, score = cuda_lib.attn_scored(k, v, q, lens=_lens(lens))
+        for s, n in enumerate(lens):
+            ref, got, tol, score_tol = scored(q[s], k[s], v[s], n, None, m, 1.0)
+            _near(out[s], ref, tol, (m, s))
+            _near(score[s, :n], got, score_tol, (m, s, "scores"))
+            assert not score[s, n:].any()
+    rows = keep_rows(score[2, :700].tolist(), range(700), 700, 100, 0, 10)
+    kept = cuda_lib.cache_evict(k, v, score, 100, lens=_lens(lens), n_recent=10)
+    assert kept["lens"].tolist() == [5, 0, 100] and kept["pos"][2].tolist() == rows
+    assert torch.equal(kept["k"][2], k[2, rows]) and torch.equal(kept["v"][2], v[2, rows])
+    n_lens = _lens(lens)
+    cuda_lib.cache_evict(k, v, score, 100, lens=n_lens, n_recent=10, in_place=True)
+    assert n_lens.tolist() == [5, 0, 100]
+    assert torch.equal(kept["k"][2], k[2, :100]) and torch.equal(kept["v"][2], v[2, :100]) and torch.equal(kept["score"][2], score[2, :100])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("m", [1, 40, 150])
 def test_scores_are_optional(cuda_lib, dtype, m):
     _check_scored(cuda_lib, dtype, 128, 4, 321, [321, 200, 0], m, 0, seed=3)
@@ -192,6 +230,23 @@ def test_eviction_of_equal_scores_and_without_positions(cuda_lib, in_place):
     _check_evict(cuda_lib, "fp32", 64, 20000, [20000, 0], 7, 0, 7, kind="spread", with_pos=False, in_place=in_place)
 
 
+def test_eviction_with_equal_positions(cuda_lib):
+    """Positions that occur more than once, all of them the newest: the lowest rows stay."""
+    k, v, score = _normal(1, 2, 300, 64), _normal(2, 2, 300, 64), _normal(3, 2, 300)
+    pos = torch.full((2, 300), 7, dtype=torch.int32, device="cuda")
+    for keep in (50, 299):
+        got = cuda_lib.cache_evict(k, v, score, keep, pos=pos, n_recent=1)
+        assert torch.equal(got["k"], k[:, :keep]) and torch.equal(got["v"], v[:, :keep]) and torch.equal(got["score"], score[:, :keep])
+        assert got["lens"].tolist() == [keep, keep]
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+def test_more_streams_than_ctas_at_once(cuda_lib, in_place):
+    """One row over a budget and short streams, by more clusters than the device holds."""
+    _check_evict(cuda_lib, "bf16", 64, 33, [33 - s % 3 for s in range(700)], 32, 2, 8, in_place=in_place)
+    _check_evict(cuda_lib, "fp32", 128, 2500, [2500 - s % 2 for s in range(200)], 2499, 2, 8, kind="spread", in_place=in_place)
+
+
 def test_eviction_into_a_larger_cache(cuda_lib):
     _check_evict(cuda_lib, "bf16", 128, 300, [300, 20], 100, 4, 10, cap_out=250)
     _check_evict(cuda_lib, "bf16", 128, 80, [80, 20], 100, 4, 10, cap_out=100)
@@ -254,6 +309,34 @@ def _check_prefix(bk, dtype, d, B, H, g, P, cap, lens, weighted, seed=0):
 ])
 def test_shared_prefix(cuda_lib, dtype, d, B, H, g, P, cap, lens, weighted):
     _check_prefix(cuda_lib, dtype, d, B, H, g, P, cap, lens, weighted, seed=B + P)
+
+
+@pytest.mark.parametrize("weighted", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("d,B,H,g,P,cap,lens", [
+    (128, 2, 2, 3, 1500, 40, [0, 33]), (64, 1, 3, 8, 3001, 0, None), (128, 4, 1, 2, 33, 2000, [2000, 1, 0, 777]), (64, 300, 2, 1, 127, 3, [b % 4 for b in range(300)]),
+])
+def test_prefix_much_longer_or_shorter_than_the_own_rows(cuda_lib, dtype, d, B, H, g, P, cap, lens, weighted):
+    _check_prefix(cuda_lib, dtype, d, B, H, g, P, cap, lens, weighted, seed=B + P)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("B", [1, 40, 200])
+def test_prefix_whose_rows_are_all_absent(cuda_lib, dtype, B):
+    """Weights of zero everywhere, over rows that hold NaN: the own rows alone, and zeros where there are none."""
+    t, H, g, P, cap, d = TYPES[dtype], 2, 4, 500, 30, 128
+    pk, w = torch.full((H, P, d), math.nan, dtype=t, device="cuda"), torch.zeros(H, P, device="cuda")
+    k, v, q = _keys(1, B, H, cap, d, dtype=t), _normal(2, B, H, cap, d, dtype=t), _normal(3, B, H * g, d, dtype=t)
+    lens = [0] + [cap] * (B - 1)
+    out = cuda_lib.decode_attn_prefix(pk, pk, k, v, q, lens=_lens(lens), weight=w)
+    assert not out[0].any()
+    for b in range(1, B, 13):
+        for h in range(H):
+            qq = q[b, h * g:(h + 1) * g]
+            ref, _, tol, _ = attention(qq, k[b, h], v[b, h], torch.ones(g, cap, dtype=torch.bool, device="cuda"), rounded_p=True)
+            _near(out[b, h * g:(h + 1) * g], ref, tol, (b, h))
+    alone = cuda_lib.decode_attn_prefix(pk, pk, None, None, q, weight=w)
+    assert bool((alone == 0).all())
 
 
 # ---------------------------------------------------------------------------------------------- as they are used
