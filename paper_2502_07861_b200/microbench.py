@@ -3,6 +3,9 @@
     python -m paper_2502_07861_b200.microbench decode   --batch 32 --cache-len 8192 --levels 2 [--two-instance]
     python -m paper_2502_07861_b200.microbench compress --streams 8 --context 32768 --block 1024 --levels 2
     python -m paper_2502_07861_b200.microbench bucket   --streams 8 --context 32768 --buckets 5
+    python -m paper_2502_07861_b200.microbench scored   --streams 8 --rows 8192 --queries 8192 [--scored 64] [--dtype fp32]
+    python -m paper_2502_07861_b200.microbench evict    --streams 256 --rows 4096 --keep 1024 [--in-place]
+    python -m paper_2502_07861_b200.microbench prefix   --batch 32 --prefix 32768 --rows 512 [--weighted]
 
 Prints one JSON line per run.  Inputs are drawn on the device (torch.randn), which is enough
 for timing; parity is the tests' job.
@@ -190,6 +193,68 @@ def run_bucket(a):
     ctx.close()
 
 
+def _timed(call, bytes_, flops, iters, **what):
+    """One JSON line: time of a call by CUDA events, and the rates of what it cannot do without."""
+    hbm, tflops, src = _peaks()
+    for _ in range(3):
+        call()
+    start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    start.record()
+    for _ in range(iters):
+        call()
+    end.record()
+    torch.cuda.synchronize()
+    us = start.elapsed_time(end) * 1e3 / iters
+    print(json.dumps(dict(**what, us_per_call=us, algorithmic_bytes=bytes_, achieved_gbs=bytes_ / us / 1e3, frac_hbm=bytes_ / us / 1e3 / hbm, algorithmic_flops=flops,
+                          achieved_tflops=flops / us / 1e6, frac_bf16=flops / us / 1e6 / tflops, peak_source=src)))
+
+
+def _rows(dtype, *shape):
+    return torch.randn(*shape, device="cuda").to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+
+
+def run_scored(a):
+    """Attention of the newest queries over caller-held caches, with the weights that the cached rows receive."""
+    S, n, g, m, d = a.streams, a.rows, a.group, a.queries, a.head_dim
+    k, v, q = _rows(a.dtype, S, n, d), _rows(a.dtype, S, n, d), _rows(a.dtype, S, g, m, d)
+    score, scored = torch.zeros(S, n, device="cuda"), m if a.scored is None else a.scored
+    seen = m * (n - m) + m * (m + 1) // 2 if n >= m else n * (n + 1) // 2
+    _timed(lambda: bk.attn_scored(k, v, q, score=score, n_scored=scored, decay=0.5), S * n * (2 * d * k.element_size() + 8) + 2 * q.numel() * q.element_size(),
+           4 * d * g * S * seen, a.iters, kernel="attn_scored", streams=S, rows=n, group=g, queries=m, scored=scored, head_dim=d, dtype=a.dtype)
+
+
+def run_evict(a):
+    """Eviction of all but the rows of most weight; in place, each call evicts from the rows that the one before has left."""
+    S, n, d = a.streams, a.rows, a.head_dim
+    k, v, score = _rows(a.dtype, S, n, d), _rows(a.dtype, S, n, d), torch.rand(S, n, device="cuda")
+    pos = torch.arange(n, dtype=torch.int32, device="cuda").repeat(S, 1)
+    lens = torch.full((S,), n, dtype=torch.int32, device="cuda")
+    full, keep = lens.clone(), min(a.keep, n)
+    kw = dict(n_first=min(4, keep), n_recent=min(64, max(0, keep - 4)))
+    if a.in_place:
+        def call():
+            lens.copy_(full)
+            bk.cache_evict(k, v, score, keep, lens=lens, pos=pos, in_place=True, **kw)
+        moved = min(keep, n - keep)
+    else:
+        out = bk.cache_evict(k, v, score, keep, lens=lens, pos=pos, **kw)
+        call = lambda: bk.cache_evict(k, v, score, keep, lens=lens, pos=pos, out=out, **kw)  # noqa: E731
+        moved = keep
+    _timed(call, S * (8 * n + 8 * moved + 4 * moved * d * k.element_size()), 0, a.iters, kernel="cache_evict", streams=S, rows=n, keep=keep, head_dim=d,
+           dtype=a.dtype, in_place=a.in_place)
+
+
+def run_prefix(a):
+    """A decode step of a batch behind a shared prefix."""
+    B, H, g, P, n, d = a.batch, a.kv_heads, a.group, a.prefix, a.rows, a.head_dim
+    pk, pv, q = _rows(a.dtype, H, P, d), _rows(a.dtype, H, P, d), _rows(a.dtype, B, H * g, d)
+    k, v = (_rows(a.dtype, B, H, n, d), _rows(a.dtype, B, H, n, d)) if n else (None, None)
+    w = torch.full((H, P), 4.0, device="cuda") if a.weighted else None
+    rows = H * (P + B * n)
+    _timed(lambda: bk.decode_attn_prefix(pk, pv, k, v, q, weight=w), 2 * rows * d * q.element_size() + 2 * q.numel() * q.element_size() + (4 * H * P if a.weighted else 0),
+           4 * d * g * H * B * (P + n), a.iters, kernel="decode_attn_prefix", batch=B, kv_heads=H, group=g, prefix=P, rows=n, weighted=a.weighted, head_dim=d, dtype=a.dtype)
+
+
 def main():
     ap = argparse.ArgumentParser()
     sub = ap.add_subparsers(dest="cmd", required=True)
@@ -225,10 +290,23 @@ def main():
     b.add_argument("--levels", type=int, default=2)
     b.add_argument("--buckets", type=int, default=5)
     b.add_argument("--iters", type=int, default=10)
+    for name, sizes in (("scored", dict(streams=8, rows=8192, queries=1, group=4)), ("evict", dict(streams=256, rows=4096, keep=1024)),
+                        ("prefix", dict(batch=32, kv_heads=8, group=4, prefix=32768, rows=512))):
+        o = sub.add_parser(name)
+        for size, value in dict(sizes, head_dim=128, iters=20).items():
+            o.add_argument("--" + size.replace("_", "-"), type=int, default=value)
+        o.add_argument("--dtype", choices=["bf16", "fp32"], default="bf16")
+        if name == "scored":
+            o.add_argument("--scored", type=int, default=None, help="newest queries that count (all)")
+        elif name == "evict":
+            o.add_argument("--in-place", action="store_true")
+        else:
+            o.add_argument("--weighted", action="store_true")
     a = ap.parse_args()
     if not torch.cuda.is_available():
         raise SystemExit("microbench needs a CUDA device")
-    {"decode": run_decode, "compress": run_compress, "bucket": run_bucket}[a.cmd](a)
+    {"decode": run_decode, "compress": run_compress, "bucket": run_bucket, "scored": run_scored, "evict": run_evict,
+     "prefix": run_prefix}[a.cmd](a)
 
 
 if __name__ == "__main__":
