@@ -523,6 +523,13 @@ def _workspace(device, size):
     return torch.empty(size, dtype=torch.uint8, device=device) if size else None
 
 
+def _in_32_bits(what, *numbers):
+    """ctypes would cut the upper bits off."""
+    for n in numbers:
+        if not -(1 << 31) <= n < 1 << 31:
+            raise ValueError(f"{what}: {n} does not fit 32 bits")
+
+
 def attn_scored(K, V, q, lens=None, score=None, score_out=None, n_scored=None, decay=1.0, out=None, stream=None):
     """Attention of every stream's newest tokens over its cache, and the weight that each cached row receives (see balancekv.h).
 
@@ -542,6 +549,7 @@ def attn_scored(K, V, q, lens=None, score=None, score_out=None, n_scored=None, d
     code = _dtype_code(what, dtype)
     if n_scored is None:
         n_scored = m
+    _in_32_bits(what, n_scored)
     if not (qs[0] == S and qs[-1] == d and _is(K, dtype, ks, device) and _is(V, dtype, ks, device) and _is(q, dtype, qs, device) and _is(out, dtype, qs, device)
             and _is(lens, torch.int32, (S,), device) and _is(score, f32, ss, device) and _is(score_out, f32, ss, device)):
         _expect(what, device, K=(K, dtype, ks), V=(V, dtype, ks), q=(q, dtype, (S, *qs[1:-1], d)), out=(out, dtype, qs), lens=(lens, torch.int32, (S,)),
@@ -572,6 +580,7 @@ def cache_evict(K, V, score, n_keep, lens=None, pos=None, n_first=0, n_recent=0,
     ks = K.shape
     if len(ks) != 3:
         raise ValueError(f"{what}: expected K [n_streams, capacity, d]")
+    _in_32_bits(what, n_keep, n_first, n_recent)
     S, cap, d = ks
     dtype, device, ss, i32, f32 = K.dtype, K.get_device(), (S, cap), torch.int32, torch.float32
     code = _dtype_code(what, dtype)

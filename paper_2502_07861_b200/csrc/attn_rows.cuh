@@ -51,8 +51,10 @@ struct AttnRows {
 __host__ __device__ inline int64_t attn_row(const AttnRows& A, int s, int r) {
   return (int64_t)s * A.q_stream + (int64_t)(r / A.q_inner) * A.q_outer + r % A.q_inner;
 }
+// Some kernels read lens, queries and old scores before they wait for the kernel ahead of them, which has waited for what wrote these:
+// past L1, whose lines may be older than that.
 __device__ inline int attn_len(const AttnRows& A, int s) {
-  return A.lens ? max(0, min(A.lens[s / A.lens_div], A.cap)) : A.cap;
+  return A.lens ? max(0, min(__ldcg(A.lens + s / A.lens_div), A.cap)) : A.cap;
 }
 // Rows that query row r of a stream of len rows sees.
 __device__ inline int attn_limit(const AttnRows& A, int len, int r) {
@@ -81,7 +83,7 @@ struct ScoreArgs {
   float decay;
   int32_t n_scored;
 };
-__device__ inline float score_old(const ScoreArgs& S, int64_t at) { return S.in ? S.in[at] : 0.f; }
+__device__ inline float score_old(const ScoreArgs& S, int64_t at) { return S.in ? __ldcg(S.in + at) : 0.f; }
 __device__ inline void score_put(const ScoreArgs& S, int64_t at, float old, float sum) { S.out[at] = S.in ? fmaf(S.decay, old, sum) : sum; }
 __device__ inline void score_put(const ScoreArgs& S, int64_t at, float sum) { score_put(S, at, score_old(S, at), sum); }
 

@@ -149,8 +149,8 @@ __device__ inline void few_warp_bf16(const AttnRows& A, const Group& G, const Lo
     const __nv_bfloat16* qp = static_cast<const __nv_bfloat16*>(A.q) + (hr < g ? attn_row(A, s, G.r0 + hr) : 0) * D;
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) {
-      qb[ks][0] = hr < g ? *reinterpret_cast<const uint32_t*>(qp + ks * 16 + 2 * tq) : 0u;
-      qb[ks][1] = hr < g ? *reinterpret_cast<const uint32_t*>(qp + ks * 16 + 8 + 2 * tq) : 0u;
+      qb[ks][0] = hr < g ? __ldcg(reinterpret_cast<const uint32_t*>(qp + ks * 16 + 2 * tq)) : 0u;
+      qb[ks][1] = hr < g ? __ldcg(reinterpret_cast<const uint32_t*>(qp + ks * 16 + 8 + 2 * tq)) : 0u;
     }
   }
   int limit[2];
@@ -449,7 +449,7 @@ __device__ inline void few_tiles(const AttnRows& A, const Group& G, const Logits
   R.start(lane);
   if constexpr (!kBf16) {
     for (int i = tid; i < kR * D; i += kThreads)
-      sh.qs[i] = i / D < G.g ? static_cast<const float*>(A.q)[attn_row(A, s, G.r0 + i / D) * D + i % D] : 0.f;
+      sh.qs[i] = i / D < G.g ? __ldcg(static_cast<const float*>(A.q) + attn_row(A, s, G.r0 + i / D) * D + i % D) : 0.f;
     __syncthreads();
   }
   float* mrg = reinterpret_cast<float*>(tiles) + warp * kFewRows * F::kPitch;

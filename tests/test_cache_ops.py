@@ -85,3 +85,14 @@ def test_tensors_off_the_device_are_refused():
         bk.attn_scored(k.half(), k.half(), torch.zeros(2, 1, 64).half())
     with pytest.raises(ValueError, match="share"):
         bk.decode_attn_prefix(k, k, None, None, torch.zeros(3, 3, 64))
+
+
+def test_numbers_beyond_32_bits_are_refused():
+    import torch
+
+    x, score = torch.zeros(2, 10, 64), torch.zeros(2, 10)
+    for change in (dict(n_keep=(1 << 32) + 5), dict(n_keep=5, n_first=1 << 32), dict(n_keep=5, n_recent=-(1 << 32))):
+        with pytest.raises(ValueError, match="32 bits"):
+            bk.cache_evict(x, x, score, **change)
+    with pytest.raises(ValueError, match="32 bits"):
+        bk.attn_scored(x, x, torch.zeros(2, 4, 1, 64), n_scored=(1 << 32) + 1)
