@@ -433,18 +433,23 @@ int blocks_of(const AttnRows& A) { return by_keys(A) ? 1 : (A.n_rows + 2 * rows_
 
 // CTAs that share the keys of a block of query rows, each an SM: the factor of the shortest time, in tiles of keys: those of a wave's CTA
 // and three for its start and end, and those that writing and joining the splits takes (fp32 rows there and back; a pair of query tiles and
-// four splits about one); two tiles of keys each at least.
+// four splits about one); two tiles of keys each at least.  Where the blocks alone fill the SMs, splits have to save a quarter by that count: an
+// idle SM leaves the others its power, and joining costs (8 x 1024 queries x 5 heads behind 32768 rows, 160 blocks: 880 us by one split, 683
+// by eight; 40 x 512 x 4 behind 8192, 320 blocks: 368 against 425; 16 x 2048 x 3 behind 30000, 384 blocks: 1435 against 1521).  Blocks of a
+// prompt differ in what they see, and even out by themselves.
 int attn_tc_splits(const AttnRows& A) {
   const int64_t blocks = (int64_t)blocks_of(A) * A.n_streams, tiles = ((int64_t)A.cap + kTcKeys - 1) / kTcKeys;
   int best = 1;
   int64_t least = INT64_MAX;
-  if (blocks >= kAttnSms) return 1;
+  if (blocks >= kAttnSms && 2 * (int64_t)A.n_queries > A.cap) return 1;
+  int64_t whole = 0;
   for (int splits = 1; splits <= kAttnMaxSplits / 2 && (splits == 1 || 2 * splits <= tiles); ++splits) {
     const int64_t time = 4 * ((blocks * splits + kAttnSms - 1) / kAttnSms * ((tiles + splits - 1) / splits + 3)) +
                          (splits > 1 ? 4 + (splits * blocks + kAttnSms - 1) / kAttnSms : 0);
+    if (splits == 1) whole = time;
     if (time < least) { least = time; best = splits; }
   }
-  return best;
+  return blocks >= kAttnSms && 4 * least > 3 * whole ? 1 : best;
 }
 // Slots of partial results that a launch of so many splits fills.
 int attn_tc_slots(const AttnRows& A, int splits) { return by_keys(A) ? 2 * splits : splits; }

@@ -87,6 +87,11 @@ def test_a_handful_of_queries(cuda_lib, dtype, d, g, cap, lens, m, n_scored):
     _check_scored(cuda_lib, dtype, d, g, cap, lens, m, n_scored, seed=cap)
 
 
+def test_a_few_more_blocks_of_queries_than_sms(cuda_lib):
+    """150 blocks of query rows, whose keys are split so that the last two do not take a second turn alone."""
+    _check_scored(cuda_lib, "bf16", 64, 4, 9000, [9000 - 120 * s for s in range(75)], 100, 7, seed=2)
+
+
 @pytest.mark.parametrize("dtype,cap", [("bf16", 6300000), ("fp32", 3200000)])
 def test_offsets_beyond_32_bits(cuda_lib, dtype, cap):
     """The last stream of caches of more than 2^32 bytes, by the one-pass kernels, the tiles and the eviction."""
