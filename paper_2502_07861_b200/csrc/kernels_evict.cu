@@ -399,8 +399,15 @@ cudaError_t launch_move(const EvictArgs& E, cudaStream_t st) {
 }  // namespace
 
 cudaError_t launch_evict(const EvictArgs& E, cudaStream_t st) {
+  // CTAs of a stream: one for each 2048 rows, while a launch has not more of them than serve it.  An SM starts clusters slowly, and what a
+  // CTA does beside reading its rows is the same for few and many.  One row over the budget, in place: a CTA an SM (256 streams of 4097 rows: 9.8 us by
+  // 256 CTAs, 17.6 by 1024; 64 of 8193: 7.3 by 128, 13.0 by 512).  Others in place: two (256 full streams of 8192: 45 us by 256, 65 by
+  // 1024; 64 of 16384: 30 by 256, 43 by 512).  Out of place, where a stream's list of sources is written too: three and a half (256 streams
+  // of up to 8192: 102 us by 512, 110 by 1024; 256 of up to 4096: 57 by 512, 60 by 256).  A CTA always keeps its rows' keys on the chip
+  // where eight can.
+  const int64_t most = E.in_place ? (E.cap - E.keep <= 1 ? kAttnSms : 2 * kAttnSms) : 7 * kAttnSms / 2;
   int C = 1;
-  while (C < kMaxCluster && E.cap > 2048 * C) C *= 2;
+  while (C < kMaxCluster && E.cap > 2048 * C && ((int64_t)2 * C * E.n_streams <= most || E.cap > kStageRows * C)) C *= 2;
   // One launch where every CTA has an SM to itself and little to copy; larger clusters share the copying.  The second launch costs the
   // host 2.5 us and the device 4; a CTA moves about 100 KB a microsecond, half of that where sources come from a list (1 stream, 4000 of 16000
   // rows by 8 CTAs with 512 KB each: 26 us against 17 by two launches; 64 streams, 1024 of 1025: 15.6 us a call against 18.2).  With more
