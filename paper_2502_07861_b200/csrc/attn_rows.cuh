@@ -184,7 +184,6 @@ cudaError_t launch_attn_few_cluster(const AttnRows& A, const ScoreArgs& S, int C
 cudaError_t launch_few_end(const AttnRows& A, float* x, const ScoreArgs& S, int d, int is_bf16, cudaStream_t st);
 
 int attn_tc_splits(const AttnRows& A);
-int attn_tc_slots(const AttnRows& A, int splits);
 cudaError_t launch_attn_tc(const AttnRows& A, int d, cudaStream_t st);
 cudaError_t launch_score_tc(const AttnRows& A, const ScoreArgs& S, int d, cudaStream_t st);
 

@@ -74,7 +74,7 @@ int plan_scored(AttnRows& A, float*& x, Pieces& ws, int n_streams, int capacity,
     return BALANCEKV_OK;
   }
   A.splits = few ? few_splits(n_streams, capacity, (int)rows, head_dim, dtype) : dtype ? attn_tc_splits(A) : simt_splits((int64_t)simt_row_tiles((int)rows) * n_streams, capacity);
-  A.n_slots = !few && dtype ? attn_tc_slots(A, A.splits) : A.splits;
+  A.n_slots = A.splits;
   take_parts(A, ws, head_dim);
   if (n_scored) A.lse = ws.take<float>(A.total_rows);
   x = n_scored && few ? ws.take<float>(A.total_rows * few_pitch(capacity)) : nullptr;
@@ -108,7 +108,7 @@ int plan_prefix(AttnRows& P, AttnRows& A, Pieces& ws, int prefix_len, int capaci
   A.cap = capacity;
   A.n_rows = A.q_stream = A.q_inner = group;
   A.splits = capacity ? few_splits(streams, capacity, group, head_dim, dtype) : 0;
-  A.slot0 = !few && dtype ? attn_tc_slots(P, P.splits) : P.splits;
+  A.slot0 = P.splits;
   P.n_slots = A.n_slots = A.slot0 + A.splits;
   take_parts(P, ws, head_dim);
   A.part = P.part;

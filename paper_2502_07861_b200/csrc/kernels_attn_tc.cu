@@ -7,7 +7,7 @@
 // writes them over S as bf16; O += P V (P from TMEM), half of the keys as soon as their weights are there.  The two tiles take turns, so
 // that the tensor core multiplies for one while the other's weights are formed: per pair of tiles the products take 2048 cycles
 // (d = 128), and so would 32768 exponentials of the special-function unit; a share of them is therefore formed by FMAs.
-// A stream with one tile of query rows has it twice, and the two take the even and the odd tiles of keys (by_keys).
+// A stream with one tile of query rows has it twice, and the two take the even and the odd tiles of keys and add their sums up (by_keys).
 // The maximum m_r is the one seen when it last grew by more than 8: weights then stay below 2^8, and O is brought to a new maximum
 // only that often (usually in the first tiles).  Sums and maxima are fp32; the weights are rounded to bf16 for the second product,
 // their sum is not.
@@ -360,33 +360,92 @@ attn_tc_kernel(const __grid_constant__ TcArgs P, const __grid_constant__ CUtenso
       tc_fence_after();
     }
     if (!ok) l = NAN;
-    const int64_t row = valid ? attn_row(A, s, r) : 0;
+    // The results leave by way of shared memory, 32 columns of a warp's rows at a time, so that neighbouring lanes write neighbouring bytes
+    // (a row per lane, 16 bytes at a time, took 8200 cycles for two tiles of sums).  Its Q tile is there for it: every S is formed.
+    uint4* const stage = reinterpret_cast<uint4*>(sm + t * Sh::kTile) + (warp % 4) * (Sh::kTile / 64);
     const bool parts = A.n_slots > 1;
-    const float inv = parts ? 1.f : l == 0.f ? 0.f : 1.f / l;
-    const int64_t at = (int64_t)(A.slot0 + (by_keys ? 2 * split + t : split)) * A.total_rows + row;
-    if (valid && parts) A.part_ml[at] = make_float2(m, l);
-    if (valid && !parts && A.lse) A.lse[row] = l == 0.f ? INFINITY : m + log2f(l);
-#pragma unroll
-    for (int c = 0; c < D; c += 32) {
-      float o[32];
-      if (mine > 0) {
+    const int row = valid ? (int)attn_row(A, s, r) : -1;
+    float top = m, sum = l, f = 1.f;             // f: of this thread's O
+    auto pair_sync = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1 + warp % 4) : "memory"); };      // the warps of the same query rows
+    const uint4* const theirs = reinterpret_cast<const uint4*>(sm + (1 - t) * Sh::kTile) + (warp % 4) * (Sh::kTile / 64);
+    if (by_keys) {                               // two sums of the same rows become one
+      reinterpret_cast<float2*>(stage)[lane] = make_float2(m, l);
+      pair_sync();
+      const float2 other = reinterpret_cast<const float2*>(theirs)[lane];
+      pair_sync();
+      top = fmaxf(m, other.x);
+      const float at = top == -INFINITY ? 0.f : top;
+      f = ex2(m - at);
+      // (added in the same order by both)
+      const float mine_l = l * f, other_l = other.y * ex2(other.x - at);
+      sum = t ? other_l + mine_l : mine_l + other_l;
+    }
+    if (valid && !(by_keys && t)) {
+      if (parts) A.part_ml[(int64_t)(A.slot0 + split) * A.total_rows + row] = make_float2(top, sum);
+      else if (A.lse) A.lse[row] = sum == 0.f ? INFINITY : top + log2f(sum);
+    }
+    if (!parts) f = sum == 0.f ? 0.f : f / sum;
+    const bool any = mine > 0;
+    auto take = [&](int c, float (&o)[32]) {
+      if (any) {
         tmem_ld32(O + c, o);
         tmem_ld_wait();
       }
 #pragma unroll
-      for (int i = 0; i < 32; ++i) o[i] = mine > 0 && l != 0.f ? o[i] * inv : 0.f;
-      if (!valid) {
-      } else if (parts) {
-        float4* to = reinterpret_cast<float4*>(A.part + at * D + c);
+      for (int i = 0; i < 32; ++i) o[i] = any && l != 0.f ? o[i] * f : 0.f;
+    };
+    auto put = [&](int c, const float (&o)[32]) {
+      __syncwarp();
+      if (parts) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) to[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+        for (int i = 0; i < 8; ++i)
+          stage[8 * lane + (i ^ (lane & 7))] = make_uint4(__float_as_uint(o[4 * i]), __float_as_uint(o[4 * i + 1]), __float_as_uint(o[4 * i + 2]), __float_as_uint(o[4 * i + 3]));
+        __syncwarp();
+        const int piece = lane % 8;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int from = 4 * i + lane / 8, to = __shfl_sync(0xffffffffu, row, from);
+          if (to >= 0) *reinterpret_cast<uint4*>(A.part + ((int64_t)(A.slot0 + split) * A.total_rows + to) * D + c + 4 * piece) = stage[8 * from + (piece ^ (from & 7))];
+        }
       } else {
-        uint4* to = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(A.out) + row * D + c);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          to[i] = make_uint4(pack_bf16(o[8 * i], o[8 * i + 1]), pack_bf16(o[8 * i + 2], o[8 * i + 3]), pack_bf16(o[8 * i + 4], o[8 * i + 5]), pack_bf16(o[8 * i + 6], o[8 * i + 7]));
+          stage[4 * lane + (i ^ (lane >> 1 & 3))] =
+              make_uint4(pack_bf16(o[8 * i], o[8 * i + 1]), pack_bf16(o[8 * i + 2], o[8 * i + 3]), pack_bf16(o[8 * i + 4], o[8 * i + 5]), pack_bf16(o[8 * i + 6], o[8 * i + 7]));
+        __syncwarp();
+        const int piece = lane % 4;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int from = 8 * i + lane / 4, to = __shfl_sync(0xffffffffu, row, from);
+          if (to >= 0) *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(A.out) + (int64_t)to * D + c + 8 * piece) = stage[4 * from + (piece ^ (from >> 1 & 3))];
+        }
       }
-      __syncwarp();
+    };
+    if (by_keys) {                               // a half of the columns each: the other half's sums to the other warp
+      constexpr int kHalf = D / 2;
+#pragma unroll
+      for (int c = 0; c < kHalf; c += 32) {
+        float o[32];
+        take(kHalf * (1 - t) + c, o);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) reinterpret_cast<float*>(stage)[32 * (c + i) + lane] = o[i];
+      }
+      float o[kHalf / 32][32];
+#pragma unroll
+      for (int c = 0; c < kHalf; c += 32) take(kHalf * t + c, o[c / 32]);
+      pair_sync();
+#pragma unroll
+      for (int c = 0; c < kHalf; ++c) o[c / 32][c % 32] += reinterpret_cast<const float*>(theirs)[32 * c + lane];
+      pair_sync();
+#pragma unroll
+      for (int c = 0; c < kHalf; c += 32) put(kHalf * t + c, o[c / 32]);
+    } else {
+#pragma unroll 1
+      for (int c = 0; c < D; c += 32) {
+        float o[32];
+        take(c, o);
+        put(c, o);
+      }
     }
     tc_fence_before();
   }
@@ -443,7 +502,7 @@ int attn_tc_splits(const AttnRows& A) {
   int64_t least = INT64_MAX;
   if (blocks >= kAttnSms && 2 * (int64_t)A.n_queries > A.cap) return 1;
   int64_t whole = 0;
-  for (int splits = 1; splits <= kAttnMaxSplits / 2 && (splits == 1 || 2 * splits <= tiles); ++splits) {
+  for (int splits = 1; splits <= kAttnMaxSplits && (splits == 1 || 2 * splits <= tiles); ++splits) {
     const int64_t time = 4 * ((blocks * splits + kAttnSms - 1) / kAttnSms * ((tiles + splits - 1) / splits + 3)) +
                          (splits > 1 ? 4 + (splits * blocks + kAttnSms - 1) / kAttnSms : 0);
     if (splits == 1) whole = time;
@@ -451,8 +510,6 @@ int attn_tc_splits(const AttnRows& A) {
   }
   return blocks >= kAttnSms && 4 * least > 3 * whole ? 1 : best;
 }
-// Slots of partial results that a launch of so many splits fills.
-int attn_tc_slots(const AttnRows& A, int splits) { return by_keys(A) ? 2 * splits : splits; }
 
 cudaError_t launch_attn_tc(const AttnRows& A, int d, cudaStream_t st) {
   const TcArgs P{A, rows_per_tile(A), A.q_outer ? 128 / A.q_inner : 0, blocks_of(A), by_keys(A)};
