@@ -177,13 +177,18 @@ cudaError_t launch_score_simt(const AttnRows& A, const ScoreArgs& S, int d, cuda
 
 int few_splits(int64_t streams, int cap, int n_rows, int d, int is_bf16);
 int64_t few_pitch(int cap);
-cudaError_t launch_attn_few(const AttnRows& A, float* x, const AttnRows* also, bool finish, int d, int is_bf16, cudaStream_t st);
+// How a launch of the one-pass kernel stands to the launch before it: behind it; behind it, to finish its outputs (one split, which joins the slots
+// before its own); beside it, on the SMs that it leaves.
+enum FewOrder { kFewAlone, kFewFinish, kFewBeside };
+cudaError_t launch_attn_few(const AttnRows& A, float* x, const AttnRows* also, FewOrder order, int d, int is_bf16, cudaStream_t st);
 int few_cluster(int64_t streams, int cap, int n_rows, int d, int is_bf16);
 int64_t few_cluster_sums(const AttnRows& A);
 cudaError_t launch_attn_few_cluster(const AttnRows& A, const ScoreArgs& S, int C, float* sums, int d, int is_bf16, cudaStream_t st);
 cudaError_t launch_few_end(const AttnRows& A, float* x, const ScoreArgs& S, int d, int is_bf16, cudaStream_t st);
 
 int attn_tc_splits(const AttnRows& A);
+int attn_tc_blocks(const AttnRows& A);         // CTAs of a split, of all streams
+bool attn_tc_by_keys(const AttnRows& A);
 cudaError_t launch_attn_tc(const AttnRows& A, int d, cudaStream_t st);
 cudaError_t launch_score_tc(const AttnRows& A, const ScoreArgs& S, int d, cudaStream_t st);
 

@@ -87,7 +87,26 @@ int plan_scored(AttnRows& A, float*& x, Pieces& ws, int n_streams, int capacity,
 // rows pay only when there are a few of them.
 bool prefix_by_few(const AttnRows& P, int dtype) { return P.n_rows <= (dtype ? kFewRows : 128); }
 
-int plan_prefix(AttnRows& P, AttnRows& A, Pieces& ws, int prefix_len, int capacity, int n_seqs, int n_kv_heads, int group, int head_dim, int dtype) {
+// Whether the sequences' own rows are read beside the tensor-core kernel's work on the prefix, which then leaves them SMs, and by how many splits
+// that works.  Times in us: a pair of query tiles with a tile of keys takes 1.7, a tile of keys by itself 1.55 (it waits for memory); the one-pass
+// kernel reads 6 MB and a wave of its CTAs takes 4.5.  The SMs are shared out by these times, the tensor-core kernel's counted half as long again,
+// since others now read too.  It costs a launch that joins, unless the own rows need one anyway: short ones finish the outputs themselves instead
+// (64 x 4 x 8 behind 32768 rows, 200 own: 52 us against 55), and where the tensor-core kernel waits for memory too, so do all that are not most of the
+// work.  (256 sequences x 5 heads x 8 behind 8192 rows: with 1024 own rows each 210 us one after the other, 192 so, 256 own rows
+// 116 and 103; 128 x 8 x 4 behind 16384, 300 own: 61 and 54; 32 x 4 x 8 behind 32768, 512 own: 44 and 48, 2048 own: 83 and 77.)
+bool prefix_beside(const AttnRows& P, const AttnRows& A, int head_dim, int& splits) {
+  const bool by_keys = attn_tc_by_keys(P);
+  const int64_t blocks = attn_tc_blocks(P), tiles = (P.cap + 127) / 128;
+  const double prefix = (double)blocks * tiles * (by_keys ? 1.55 : 1.7) / kAttnSms;
+  const int64_t waves = ((int64_t)A.n_streams * A.splits + 2 * kAttnSms - 1) / (2 * kAttnSms);
+  const double own = std::max((double)A.n_streams * A.cap * head_dim * 4 / 6e6, 4.5 * waves);
+  if (A.splits == 1 && (own < 10 || (by_keys && own < 1.5 * prefix))) return false;
+  const double sms = kAttnSms * 1.5 * prefix / (1.5 * prefix + own);
+  splits = (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)std::ceil(sms / blocks), tiles / 2, kAttnMaxSplits}));
+  return true;
+}
+
+int plan_prefix(AttnRows& P, AttnRows& A, bool& beside, Pieces& ws, int prefix_len, int capacity, int n_seqs, int n_kv_heads, int group, int head_dim, int dtype) {
   if (prefix_len < 1 || capacity < 0 || n_seqs < 1 || n_kv_heads < 1 || group < 1 || group > kMaxGroup || !shape_ok(head_dim, dtype)) return BALANCEKV_E_INVAL;
   const int64_t streams = (int64_t)n_seqs * n_kv_heads;
   if (streams > kMostRows / group || streams * ((capacity + 63) / 64) > kMostRows || (int64_t)n_kv_heads * ((prefix_len + 63) / 64) > kMostRows)
@@ -108,6 +127,7 @@ int plan_prefix(AttnRows& P, AttnRows& A, Pieces& ws, int prefix_len, int capaci
   A.cap = capacity;
   A.n_rows = A.q_stream = A.q_inner = group;
   A.splits = capacity ? few_splits(streams, capacity, group, head_dim, dtype) : 0;
+  beside = capacity && dtype && !few && prefix_beside(P, A, head_dim, P.splits);
   A.slot0 = P.splits;
   P.n_slots = A.n_slots = A.slot0 + A.splits;
   take_parts(P, ws, head_dim);
@@ -170,7 +190,7 @@ extern "C" int balancekv_attn_scored(const void* K, const void* V, const int32_t
   if (const int C = cluster_of(A, n_scored, head_dim, dtype)) {
     e = launch_attn_few_cluster(A, S, C, x, head_dim, dtype, st);
   } else if (A.n_rows <= kFewRows) {
-    e = launch_attn_few(A, x, nullptr, false, head_dim, dtype, st);
+    e = launch_attn_few(A, x, nullptr, kFewAlone, head_dim, dtype, st);
     if (e == cudaSuccess && n_scored) e = launch_few_end(A, x, S, head_dim, dtype, st);
     else if (e == cudaSuccess && A.n_slots > 1) e = launch_attn_combine(A, head_dim, dtype, st);
   } else {
@@ -185,8 +205,9 @@ extern "C" int balancekv_decode_attn_prefix_workspace(int prefix_len, int capaci
                                                       size_t* bytes) {
   if (!bytes) return BALANCEKV_E_INVAL;
   AttnRows P{}, A{};
+  bool beside;
   Pieces ws{nullptr};
-  const int rc = plan_prefix(P, A, ws, prefix_len, capacity, n_seqs, n_kv_heads, group, head_dim, dtype);
+  const int rc = plan_prefix(P, A, beside, ws, prefix_len, capacity, n_seqs, n_kv_heads, group, head_dim, dtype);
   if (rc == BALANCEKV_OK) *bytes = ws.used;
   return rc;
 }
@@ -199,8 +220,9 @@ extern "C" int balancekv_decode_attn_prefix(const void* K_prefix, const void* V_
       !aligned(w_prefix, 4) || !aligned(lens, 4) || !aligned(workspace, 256))
     return BALANCEKV_E_INVAL;
   AttnRows P{}, A{};
+  bool beside;
   Pieces ws{static_cast<char*>(workspace)};
-  if (const int rc = plan_prefix(P, A, ws, prefix_len, capacity, n_seqs, n_kv_heads, group, head_dim, dtype)) return rc;
+  if (const int rc = plan_prefix(P, A, beside, ws, prefix_len, capacity, n_seqs, n_kv_heads, group, head_dim, dtype)) return rc;
   if (ws.used && !workspace) return BALANCEKV_E_INVAL;
   if (workspace_bytes < ws.used) return BALANCEKV_E_NOMEM;
   P.K = K_prefix;
@@ -212,14 +234,14 @@ extern "C" int balancekv_decode_attn_prefix(const void* K_prefix, const void* V_
   P.q = A.q = q;
   P.out = A.out = out;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  // Own rows of one split join the prefix's slots themselves (32 sequences behind 32768 rows: 54 us with a launch for that, 50.8 without).
-  const bool few = prefix_by_few(P, dtype), finish = !few && A.splits == 1 && A.slot0 <= kAttnMaxSplits;
+  // Own rows of one split join the prefix's slots themselves, unless they are read beside its launch.
+  const bool few = prefix_by_few(P, dtype), finish = !few && A.splits == 1 && !beside && A.slot0 <= kAttnMaxSplits;
   cudaError_t e;
   if (few) {
-    e = launch_attn_few(P, nullptr, A.splits ? &A : nullptr, false, head_dim, dtype, st);
+    e = launch_attn_few(P, nullptr, A.splits ? &A : nullptr, kFewAlone, head_dim, dtype, st);
   } else {
     e = dtype ? launch_attn_tc(P, head_dim, st) : launch_attn_simt(P, head_dim, st);
-    if (e == cudaSuccess && A.splits) e = launch_attn_few(A, nullptr, nullptr, finish, head_dim, dtype, st);
+    if (e == cudaSuccess && A.splits) e = launch_attn_few(A, nullptr, nullptr, finish ? kFewFinish : beside ? kFewBeside : kFewAlone, head_dim, dtype, st);
   }
   if (e == cudaSuccess && P.n_slots > 1 && !finish) e = launch_attn_combine(P, head_dim, dtype, st);
   return report("balancekv_decode_attn_prefix", e);

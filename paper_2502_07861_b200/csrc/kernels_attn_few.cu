@@ -57,7 +57,7 @@ struct FewJobs {
   int32_t groups[2];      // of query rows
   int32_t least[2];       // tiles of a CTA, where the stream has them: of shorter streams the last splits are left empty
   int32_t ctas0;          // CTAs of the first set
-  int32_t finish;         // one set of one split: the slots before its own are complete, and it joins them itself
+  int32_t order;          // FewOrder
 };
 struct FewMaps {
   CUtensorMap k[2], v[2];
@@ -579,27 +579,29 @@ __global__ void __launch_bounds__(kThreads, (Few<kBf16, D>::kCtas)) attn_few_ker
   constexpr int kGroup = group_rows(kBf16, D);
   const Group G{group * kGroup, min(kGroup, A.n_rows - group * kGroup)};
   few_init(sh, maps.k[which], maps.v[which]);
-  // A launch that finishes the outputs follows the prefix's: until it joins their slots it reads nothing that writes, so that its CTAs start as
-  // the others leave.  (What came before the prefix's launch is complete: that releases its dependents behind its own wait.)
-  if (!J.finish) grid_wait_and_release();
+  // A launch beside or behind the prefix's reads nothing that that writes, until it joins its slots, and nothing that came before is still to
+  // be written: the prefix's launch releases its dependents behind its own wait.
+  const bool early = J.order != kFewAlone;
+  if (!early) grid_wait_and_release();
   __syncthreads();
   const int len = attn_len(A, s), n_all = (len + kTile - 1) / kTile;
   const int used = max(1, min(A.splits, (n_all + J.least[which] - 1) / J.least[which]));      // splits
   if (split >= used) {
     if (warp == 0 && lane < G.g) A.part_ml[(int64_t)(A.slot0 + split) * A.total_rows + attn_row(A, s, G.r0 + lane)] = make_float2(-INFINITY, 0.f);
+    if (early && blockIdx.x == gridDim.x - 1) grid_wait_and_release();
     return;
   }
   const int64_t pitch = J.job[which].pitch;
   const Logits X{J.job[which].x ? J.job[which].x + ((int64_t)s * A.n_rows + G.r0) * pitch : nullptr, pitch};
   few_tiles(A, G, X, maps.k[which], maps.v[which], sh, tiles, s, len, (int)((int64_t)n_all * split / used), (int)((int64_t)n_all * (split + 1) / used));
   const float* mrg = reinterpret_cast<const float*>(tiles);
-  if (J.finish) grid_wait_and_release();
+  if (J.order == kFewFinish) grid_wait_and_release();
   for (int r = warp; r < G.g; r += kWarps) {
     float acc[D / 32], top, sum;
     few_join<D, kWarps>(kWarps, lane, [&](int w) { return mrg + (w * kFewRows + r) * F::kPitch; }, acc, top, sum);
     if (sh.abort_flag) sum = NAN;
     const int64_t row = attn_row(A, s, G.r0 + r);
-    if (J.finish) {
+    if (J.order == kFewFinish) {
       join_before<D>(A, row, lane, acc, top, sum);
       few_put<kBf16, D>(A, row, lane, acc, sum);
       continue;
@@ -614,6 +616,8 @@ __global__ void __launch_bounds__(kThreads, (Few<kBf16, D>::kCtas)) attn_few_ker
     if (A.lse && lane == 0) A.lse[row] = sum == 0.f ? INFINITY : (top == -INFINITY ? 0.f : top) + log2f(sum);
     few_put<kBf16, D>(A, row, lane, acc, sum);
   }
+  // The launch ends behind the prefix's, so that what waits for the one has both: one CTA waits.
+  if (J.order == kFewBeside && blockIdx.x == gridDim.x - 1) grid_wait_and_release();
 }
 
 // The splits of a stream as a cluster of CTAs, where its logits fit their shared memory: they join their sums through it, every
@@ -788,10 +792,10 @@ cudaError_t for_rows(int n_rows, Run run) {
 }
 
 template <bool kBf16, int D>
-cudaError_t launch_few(const FewArgs& P, const FewArgs* also, bool finish, cudaStream_t st) {
+cudaError_t launch_few(const FewArgs& P, const FewArgs* also, FewOrder order, cudaStream_t st) {
   using F = Few<kBf16, D>;
   FewJobs J{};
-  J.finish = finish;
+  J.order = order;
   FewMaps maps;
   int64_t ctas = 0;
   int most = 0;
@@ -889,11 +893,10 @@ int64_t few_cluster_sums(const AttnRows& A) { return A.n_rows > kFewRows ? (int6
 int64_t few_pitch(int cap) { return ((int64_t)cap + 31) / 32 * 32; }
 
 // x: [n_streams, n_rows, few_pitch(cap)] where launch_few_end is to follow, else null.  `also`: a second set of streams of the same call.
-// finish (one split): the outputs, joined with the slots of the launches before.
-cudaError_t launch_attn_few(const AttnRows& A, float* x, const AttnRows* also, bool finish, int d, int is_bf16, cudaStream_t st) {
+cudaError_t launch_attn_few(const AttnRows& A, float* x, const AttnRows* also, FewOrder order, int d, int is_bf16, cudaStream_t st) {
   const FewArgs P{A, x, few_pitch(A.cap)}, Q{also ? *also : A, nullptr, 0}, *second = also ? &Q : nullptr;
-  if (is_bf16) return d == 128 ? launch_few<true, 128>(P, second, finish, st) : launch_few<true, 64>(P, second, finish, st);
-  return d == 128 ? launch_few<false, 128>(P, second, finish, st) : launch_few<false, 64>(P, second, finish, st);
+  if (is_bf16) return d == 128 ? launch_few<true, 128>(P, second, order, st) : launch_few<true, 64>(P, second, order, st);
+  return d == 128 ? launch_few<false, 128>(P, second, order, st) : launch_few<false, 64>(P, second, order, st);
 }
 
 // Outputs and scores by clusters of C CTAs.

@@ -490,6 +490,9 @@ int blocks_of(const AttnRows& A) { return by_keys(A) ? 1 : (A.n_rows + 2 * rows_
 
 }  // namespace
 
+int attn_tc_blocks(const AttnRows& A) { return blocks_of(A) * A.n_streams; }
+bool attn_tc_by_keys(const AttnRows& A) { return by_keys(A); }
+
 // CTAs that share the keys of a block of query rows, each an SM: the factor of the shortest time, in tiles of keys: those of a wave's CTA
 // and three for its start and end, and those that writing and joining the splits takes (fp32 rows there and back; a pair of query tiles and
 // four splits about one); two tiles of keys each at least.  Where the blocks alone fill the SMs, splits have to save a quarter by that count: an
@@ -497,7 +500,7 @@ int blocks_of(const AttnRows& A) { return by_keys(A) ? 1 : (A.n_rows + 2 * rows_
 // by eight; 40 x 512 x 4 behind 8192, 320 blocks: 368 against 425; 16 x 2048 x 3 behind 30000, 384 blocks: 1435 against 1521).  Blocks of a
 // prompt differ in what they see, and even out by themselves.
 int attn_tc_splits(const AttnRows& A) {
-  const int64_t blocks = (int64_t)blocks_of(A) * A.n_streams, tiles = ((int64_t)A.cap + kTcKeys - 1) / kTcKeys;
+  const int64_t blocks = attn_tc_blocks(A), tiles = ((int64_t)A.cap + kTcKeys - 1) / kTcKeys;
   int best = 1;
   int64_t least = INT64_MAX;
   if (blocks >= kAttnSms && 2 * (int64_t)A.n_queries > A.cap) return 1;

@@ -325,6 +325,14 @@ def test_prefix_much_longer_or_shorter_than_the_own_rows(cuda_lib, dtype, d, B, 
     _check_prefix(cuda_lib, dtype, d, B, H, g, P, cap, lens, weighted, seed=B + P)
 
 
+@pytest.mark.parametrize("weighted", [False, True])
+@pytest.mark.parametrize("d,B,H,g,P,cap", [(128, 200, 4, 3, 900, 150), (64, 20, 4, 5, 3000, 900), (128, 33, 2, 4, 5000, 1300), (64, 700, 1, 2, 1500, 60)])
+def test_own_rows_beside_the_prefix(cuda_lib, d, B, H, g, P, cap, weighted):
+    """Own rows that are read while the prefix's products are formed, call after call in the same memory, with lengths of every kind."""
+    for call in range(3):
+        _check_prefix(cuda_lib, "bf16", d, B, H, g, P, cap, [(31 * b * (call + 1)) % (cap + 1) for b in range(B)], weighted, seed=B + call)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("B", [1, 40, 200])
 def test_prefix_whose_rows_are_all_absent(cuda_lib, dtype, B):
