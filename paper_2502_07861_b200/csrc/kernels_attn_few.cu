@@ -5,10 +5,10 @@
 // and where the rows are scored, the weights of every cached row: they need the finished sums of all splits, so the logits leave as
 // fp32 (4 bytes per row and query against 2 d elements read) and a second launch turns them into weights while it joins the splits.
 //
-// A CTA takes up to eight query rows and is four warps, each with a ring of its own of tiles of 32 rows that TMA fills (K and V tiles in turn, boxes of 128 bytes x
+// A CTA takes up to eight query rows and is four warps (or two, few_warps), each with a ring of its own of tiles of 32 rows that TMA fills (K and V tiles in turn, boxes of 128 bytes x
 // 32 rows, 128-byte swizzle): a warp waits for nothing but its own copies, and the lane that asks for the next tile does so as soon as
 // its warp has read the last.  bf16 tiles go through mma.sync with the cached rows as the M dimension and the queries as the eight
-// columns; fp32 tiles through FFMA, a lane per row for the logits and d / 32 columns per lane for the sums.
+// columns; fp32 tiles through packed FFMA.
 // A bounded wait that gives up makes the results NaN.
 #include <cooperative_groups.h>
 
@@ -26,7 +26,7 @@ namespace {
 
 using namespace mma;
 
-constexpr int kWarps = 4, kThreads = 32 * kWarps;
+constexpr int kWarps = 4, kThreads = 32 * kWarps;      // of the clusters' CTAs; attn_few_kernel's: few_warps
 constexpr int kTile = 32;                        // rows
 constexpr float kGrow = 8.f;                     // a maximum follows when it would grow by more: weights stay below 2^8
 constexpr uint32_t kBox = kTile * 128;           // bytes
@@ -40,11 +40,14 @@ struct Few {
   static constexpr int kEsz = kBf16 ? 2 : 4, kBoxDims = 128 / kEsz, kBoxes = D / kBoxDims;
   static constexpr uint32_t kTileBytes = kBoxes * kBox;
   static constexpr int kRing = kTileBytes == 4096 ? 6 : 3;                   // tiles of a warp in flight
-  static constexpr int kCtas = kTileBytes == 16384 ? 1 : 2;                  // that share an SM
+  static constexpr int kCtas = kTileBytes == 16384 ? 1 : 2;                  // of four warps that share an SM
   static constexpr int kPitch = D + 4;                                       // of a row in the merge buffer: sums, maximum, sum of weights
   static constexpr size_t kSmem = 1024 + (size_t)kWarps * kRing * kTileBytes;
-  static_assert(kWarps * kFewRows * kPitch * 4 <= (int)(kWarps * kRing * kTileBytes), "the merge buffer takes the rings' place");
+  static_assert(kFewRows * kPitch * 4 <= (int)(kRing * kTileBytes), "the merge buffer takes the rings' place");
 };
+// Warps of a CTA of attn_few_kernel, so that two share an SM and one starts or ends while the other reads (fp32 rows of 128 dims, 1024 streams of up
+// to 512 rows: 85 us by four warps, 77 by two; 2048 of 64, five query rows: 188 and 124).
+__host__ __device__ constexpr int few_warps(bool bf16, int d) { return !bf16 && d == 128 ? 2 : kWarps; }
 
 struct FewArgs {
   AttnRows A;
@@ -72,9 +75,9 @@ struct Logits {
   int64_t pitch;
 };
 
-// This warp's tiles of the CTA's share: every fourth of [t0, t1) from t0 + warp on.  Tile number n of the warp has the ring's
+// This warp's tiles of the CTA's share: every W-th (a warp of the CTA each) of [t0, t1) from t0 + warp on.  Tile number n of the warp has the ring's
 // entries 2 n (K) and 2 n + 1 (V).
-template <bool kBf16, int D>
+template <bool kBf16, int D, int W>
 struct Ring {
   using F = Few<kBf16, D>;
   const CUtensorMap *mk, *mv;
@@ -84,7 +87,7 @@ struct Ring {
 
   __device__ void issue(int e) const {           // one lane
     const CUtensorMap* map = e & 1 ? mv : mk;
-    const int s = e % F::kRing, row = (first_tile + (e >> 1) * kWarps) * kTile;
+    const int s = e % F::kRing, row = (first_tile + (e >> 1) * W) * kTile;
     tc::mbar_expect_tx(full + s, F::kTileBytes);
 #pragma unroll
     for (int b = 0; b < F::kBoxes; ++b) tma_load_3d(tiles + s * F::kTileBytes + b * kBox, map, b * F::kBoxDims, row, stream, full + s);
@@ -135,8 +138,8 @@ struct TileWeights {
 };
 
 // The warp's sums of its tiles, to mrg[row][kPitch].
-template <int D>
-__device__ inline void few_warp_bf16(const AttnRows& A, const Group& G, const Logits& X, const Ring<true, D>& R, int s, int len, int n_tiles, int lane, int* abort_flag,
+template <int D, int W>
+__device__ inline void few_warp_bf16(const AttnRows& A, const Group& G, const Logits& X, const Ring<true, D, W>& R, int s, int len, int n_tiles, int lane, int* abort_flag,
                                      float* mrg, bool& failed) {
   const int g = G.g;
   // With up to four rows the columns 4-7 repeat the rows 0-3, and in the second product they carry the low parts of the weights:
@@ -169,13 +172,13 @@ __device__ inline void few_warp_bf16(const AttnRows& A, const Group& G, const Lo
   const int mi = lane >> 3, mr = lane & 7;
   const int k_row = (mi & 1) * 8 + mr, k_piece = mi >> 1;
   const int v_row = (mi >> 1) * 8 + mr, v_piece = mi & 1;
-  TileWeights W{A.w ? A.w + (int64_t)s * A.cap : nullptr};
-  W.ask(R.first_tile * kTile + lane, len);
+  TileWeights weights{A.w ? A.w + (int64_t)s * A.cap : nullptr};
+  weights.ask(R.first_tile * kTile + lane, len);
   for (int n = 0; n < n_tiles; ++n) {
-    const int row0 = (R.first_tile + n * kWarps) * kTile, rows = min(kTile, len - row0);
+    const int row0 = (R.first_tile + n * W) * kTile, rows = min(kTile, len - row0);
     float log_w;
-    const uint32_t alive = W.take(rows, log_w);
-    W.ask(row0 + kWarps * kTile + lane, len);
+    const uint32_t alive = weights.take(rows, log_w);
+    weights.ask(row0 + W * kTile + lane, len);
     if (!R.wait(2 * n, lane, abort_flag)) { R.drain(2 * n, lane); failed = true; break; }
     const uint32_t Kt = tc::smem_u32(R.at(2 * n));
     float sa[2][4][4];
@@ -288,8 +291,8 @@ __device__ inline void few_warp_bf16(const AttnRows& A, const Group& G, const Lo
 // sets that take every kT-th row, each lane a part of the columns.  (A lane per row with the queries read from shared memory, and all
 // lanes on every row of V: 4300 cycles a tile of d = 64 and four queries.)
 // qs: [kR][D]; ps: [kR][32] of this warp.
-template <int D, int kR>
-__device__ inline void few_warp_fp32(const AttnRows& A, const Group& G, const Logits& X, const Ring<false, D>& R, int s, int len, int n_tiles, int lane, int* abort_flag,
+template <int D, int kR, int W>
+__device__ inline void few_warp_fp32(const AttnRows& A, const Group& G, const Logits& X, const Ring<false, D, W>& R, int s, int len, int n_tiles, int lane, int* abort_flag,
                                      const float* qs, float* ps, float* mrg, bool& failed) {
   const int g = G.g;
   constexpr int kAtOnce = kR < 4 ? kR : 4;       // queries whose logits are formed together; of more, they come from shared memory for each tile
@@ -321,13 +324,13 @@ __device__ inline void few_warp_fp32(const AttnRows& A, const Group& G, const Lo
   // piece c of this lane's columns: box and place of it
   const int set = lane / kLanes, in_set = lane % kLanes;
   auto piece = [&](int c) { return (in_set & 7) + 8 * ((in_set >> 3) + c * (kLanes / 8)); };
-  TileWeights W{A.w ? A.w + (int64_t)s * A.cap : nullptr};
-  W.ask(R.first_tile * kTile + lane, len);
+  TileWeights weights{A.w ? A.w + (int64_t)s * A.cap : nullptr};
+  weights.ask(R.first_tile * kTile + lane, len);
   for (int n = 0; n < n_tiles; ++n) {
-    const int row0 = (R.first_tile + n * kWarps) * kTile, row = row0 + lane;
+    const int row0 = (R.first_tile + n * W) * kTile, row = row0 + lane;
     float log_w;
-    const uint32_t alive = W.take(len - row0, log_w);
-    W.ask(row + kWarps * kTile, len);
+    const uint32_t alive = weights.take(len - row0, log_w);
+    weights.ask(row + W * kTile, len);
     if (!R.wait(2 * n, lane, abort_flag)) { R.drain(2 * n, lane); failed = true; break; }
     const unsigned char* Kt = R.at(2 * n);
     float x[kR];
@@ -430,42 +433,42 @@ __device__ inline void few_warp_fp32(const AttnRows& A, const Group& G, const Lo
 }
 
 // What a CTA needs in shared memory besides the rings.
-template <bool kBf16, int D, int kR>
+template <bool kBf16, int D, int kR, int W>
 struct FewShared {
-  uint64_t full[kWarps][Few<kBf16, D>::kRing];
+  uint64_t full[W][Few<kBf16, D>::kRing];
   int abort_flag;
   __align__(16) float qs[kBf16 ? 4 : kR * D];
-  __align__(16) float ps[kBf16 ? 4 : kWarps * kR * 32];
+  __align__(16) float ps[kBf16 ? 4 : W * kR * 32];
 };
 
 // The CTA's share [t0, t1) of the tiles: every warp's sums, to mrg[warp][row][kPitch] in the rings' place.
-template <bool kBf16, int D, int kR>
-__device__ inline void few_tiles(const AttnRows& A, const Group& G, const Logits& X, const CUtensorMap& mk, const CUtensorMap& mv, FewShared<kBf16, D, kR>& sh, unsigned char* tiles,
+template <bool kBf16, int D, int kR, int W>
+__device__ inline void few_tiles(const AttnRows& A, const Group& G, const Logits& X, const CUtensorMap& mk, const CUtensorMap& mv, FewShared<kBf16, D, kR, W>& sh, unsigned char* tiles,
                                  int s, int len, int t0, int t1) {
   using F = Few<kBf16, D>;
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
-  const int n_tiles = max(0, (t1 - t0 - warp + kWarps - 1) / kWarps);
-  const Ring<kBf16, D> R{&mk, &mv, tiles + warp * F::kRing * F::kTileBytes, sh.full[warp], s, t0 + warp, 2 * n_tiles};
+  const int n_tiles = max(0, (t1 - t0 - warp + W - 1) / W);
+  const Ring<kBf16, D, W> R{&mk, &mv, tiles + warp * F::kRing * F::kTileBytes, sh.full[warp], s, t0 + warp, 2 * n_tiles};
   R.start(lane);
   if constexpr (!kBf16) {
-    for (int i = tid; i < kR * D; i += kThreads)
+    for (int i = tid; i < kR * D; i += 32 * W)
       sh.qs[i] = i / D < G.g ? __ldcg(static_cast<const float*>(A.q) + attn_row(A, s, G.r0 + i / D) * D + i % D) : 0.f;
     __syncthreads();
   }
   float* mrg = reinterpret_cast<float*>(tiles) + warp * kFewRows * F::kPitch;
   bool failed = false;
-  if constexpr (kBf16) few_warp_bf16<D>(A, G, X, R, s, len, n_tiles, lane, &sh.abort_flag, mrg, failed);
-  else few_warp_fp32<D, kR>(A, G, X, R, s, len, n_tiles, lane, &sh.abort_flag, sh.qs, sh.ps + warp * kR * 32, mrg, failed);
+  if constexpr (kBf16) few_warp_bf16<D, W>(A, G, X, R, s, len, n_tiles, lane, &sh.abort_flag, mrg, failed);
+  else few_warp_fp32<D, kR, W>(A, G, X, R, s, len, n_tiles, lane, &sh.abort_flag, sh.qs, sh.ps + warp * kR * 32, mrg, failed);
   if (failed && lane == 0) tc::st_release(&sh.abort_flag, 1);
   __syncthreads();
 }
 
-template <bool kBf16, int D, int kR>
-__device__ inline void few_init(FewShared<kBf16, D, kR>& sh, const CUtensorMap& mk, const CUtensorMap& mv) {
+template <bool kBf16, int D, int kR, int W>
+__device__ inline void few_init(FewShared<kBf16, D, kR, W>& sh, const CUtensorMap& mk, const CUtensorMap& mv) {
   if (threadIdx.x != 0) return;
   asm volatile("prefetch.tensormap [%0];" ::"l"(&mk) : "memory");
   asm volatile("prefetch.tensormap [%0];" ::"l"(&mv) : "memory");
-  for (int i = 0; i < kWarps * Few<kBf16, D>::kRing; ++i) tc::mbar_init(&sh.full[0][0] + i, 1);
+  for (int i = 0; i < W * Few<kBf16, D>::kRing; ++i) tc::mbar_init(&sh.full[0][0] + i, 1);
   sh.abort_flag = 0;
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -566,10 +569,11 @@ __device__ inline void join_before(const AttnRows& A, int64_t row, int lane, flo
 
 // kR: rows that the fp32 form takes (bf16: 8).
 template <bool kBf16, int D, int kR>
-__global__ void __launch_bounds__(kThreads, (Few<kBf16, D>::kCtas)) attn_few_kernel(const __grid_constant__ FewJobs J, const __grid_constant__ FewMaps maps) {
+__global__ void __launch_bounds__(32 * few_warps(kBf16, D), 2) attn_few_kernel(const __grid_constant__ FewJobs J, const __grid_constant__ FewMaps maps) {
   using F = Few<kBf16, D>;
+  constexpr int W = few_warps(kBf16, D);
   extern __shared__ unsigned char smem_raw[];
-  __shared__ FewShared<kBf16, D, kR> sh;
+  __shared__ FewShared<kBf16, D, kR, W> sh;
   unsigned char* tiles = smem_raw + (-tc::smem_u32(smem_raw) & 1023u);
   const int which = (int)blockIdx.x >= J.ctas0, cta = blockIdx.x - (which ? J.ctas0 : 0);
   const AttnRows& A = J.job[which].A;
@@ -596,9 +600,9 @@ __global__ void __launch_bounds__(kThreads, (Few<kBf16, D>::kCtas)) attn_few_ker
   few_tiles(A, G, X, maps.k[which], maps.v[which], sh, tiles, s, len, (int)((int64_t)n_all * split / used), (int)((int64_t)n_all * (split + 1) / used));
   const float* mrg = reinterpret_cast<const float*>(tiles);
   if (J.order == kFewFinish) grid_wait_and_release();
-  for (int r = warp; r < G.g; r += kWarps) {
+  for (int r = warp; r < G.g; r += W) {
     float acc[D / 32], top, sum;
-    few_join<D, kWarps>(kWarps, lane, [&](int w) { return mrg + (w * kFewRows + r) * F::kPitch; }, acc, top, sum);
+    few_join<D, W>(W, lane, [&](int w) { return mrg + (w * kFewRows + r) * F::kPitch; }, acc, top, sum);
     if (sh.abort_flag) sum = NAN;
     const int64_t row = attn_row(A, s, G.r0 + r);
     if (J.order == kFewFinish) {
@@ -633,7 +637,7 @@ attn_few_cluster_kernel(const __grid_constant__ AttnRows A, const ScoreArgs S, i
   namespace cg = cooperative_groups;
   using F = Few<kBf16, D>;
   extern __shared__ unsigned char smem_raw[];
-  __shared__ FewShared<kBf16, D, kR> sh;
+  __shared__ FewShared<kBf16, D, kR, kWarps> sh;
   __shared__ float lse[kFewRows];
   unsigned char* tiles = smem_raw + (-tc::smem_u32(smem_raw) & 1023u);
   float* x = reinterpret_cast<float*>(tiles + kWarps * F::kRing * F::kTileBytes);      // [g][pitch]
@@ -806,7 +810,7 @@ cudaError_t launch_few(const FewArgs& P, const FewArgs* also, FewOrder order, cu
     if (e != cudaSuccess) return e;
     J.groups[i] = (A.n_rows + group_rows(kBf16, D) - 1) / group_rows(kBf16, D);
     const int64_t mine = (int64_t)J.groups[i] * A.splits * A.n_streams;
-    J.least[i] = kWarps * (mine > 4 * kAttnSms ? 8 : 1);
+    J.least[i] = few_warps(kBf16, D) * (mine > 4 * kAttnSms ? 8 : 1);
     ctas += mine;
     if (i == 0) J.ctas0 = (int)ctas;
     most = std::max(most, A.n_rows);
@@ -819,9 +823,11 @@ cudaError_t launch_few(const FewArgs& P, const FewArgs* also, FewOrder order, cu
   return for_rows<kBf16, group_rows(kBf16, D)>(most, [&](auto rows) {
     auto kern = attn_few_kernel<kBf16, D, decltype(rows)::value>;
     static std::atomic<unsigned long long> devices{0};
-    const cudaError_t e = kernel_limits(kern, F::kSmem, devices);
+    constexpr int W = few_warps(kBf16, D);
+    constexpr size_t smem = 1024 + (size_t)W * F::kRing * F::kTileBytes;
+    const cudaError_t e = kernel_limits(kern, smem, devices);
     if (e != cudaSuccess) return e;
-    const PdlConfig pc(dim3((unsigned)ctas), kThreads, F::kSmem, st);
+    const PdlConfig pc(dim3((unsigned)ctas), 32 * W, smem, st);
     return cudaLaunchKernelEx(&pc.cfg, kern, J, maps);
   });
 }
@@ -870,7 +876,8 @@ cudaError_t launch_end(const FewArgs& P, const ScoreArgs& S, cudaStream_t st) {
 // rows, up to six times as many, so that streams of different lengths even out (256 streams of up to 8192 rows: 104.9 us by 5 splits, 102.2 by 7).
 int few_splits(int64_t streams, int cap, int n_rows, int d, int is_bf16) {
   const int64_t sets = streams * ((n_rows + group_rows(is_bf16, d) - 1) / group_rows(is_bf16, d));
-  const int64_t fill = std::min<int64_t>(2 * kAttnSms / sets, (cap + kWarps * kTile - 1) / (kWarps * kTile));
+  const int share = few_warps(is_bf16, d) * kTile;
+  const int64_t fill = std::min<int64_t>(2 * kAttnSms / sets, (cap + share - 1) / share);
   const int64_t even = std::min<int64_t>((12 * kAttnSms + sets - 1) / sets, cap / 1024);
   return (int)std::max<int64_t>(1, std::min<int64_t>(std::max(fill, even), kAttnMaxSplits));
 }
