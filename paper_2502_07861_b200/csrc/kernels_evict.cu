@@ -38,7 +38,7 @@ struct SelectShared {
   int warp_a[kWarps], warp_b[kWarps];
   int cta[3][2];                                 // what the cluster's CTAs tell one another, a place per exchange
   int before_a, before_b, all_a;                 // of the CTAs before this one; of all
-  int digit, above;
+  int digit, above, equal;
   unsigned long long warp_least[kWarps], cta_least;
 };
 
@@ -112,9 +112,10 @@ __device__ inline void copy_rows(const EvictArgs& E, int s, int rows, int at, in
   }
 }
 
-// kFused: the clusters copy their streams' rows themselves.
-template <bool kFused>
-__global__ void __launch_bounds__(kThreads) evict_select_kernel(const EvictArgs E, int per, int staged) {
+// kFused: the clusters copy their streams' rows themselves.  kCtas of them are to share an SM (0: with the registers that they would like, two),
+// which serves launches of more CTAs than two an SM (256 streams of up to 4096 rows, 512 CTAs: 57 us by three, 62 by two; 2 streams of 4000: 15.4 by three, 13.4 by two).
+template <bool kFused, int kCtas>
+__global__ void __launch_bounds__(kThreads, kCtas) evict_select_kernel(const EvictArgs E, int per, int staged) {
   extern __shared__ uint32_t keys[];             // [per], behind them the positions (E.pos) [per]
   __shared__ SelectShared sh;
   cg::cluster_group cluster = cg::this_cluster();
@@ -275,11 +276,12 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const EvictArgs 
         lo += b < C ? (int)h[b].x : 0;
       }
       const int at = lane_of(hi + lo, need - before, rest);
-      const int first_hi = __shfl_sync(0xffffffffu, hi, at);
+      const int first_hi = __shfl_sync(0xffffffffu, hi, at), first_lo = __shfl_sync(0xffffffffu, lo, at);
       const bool low = need - before - rest > first_hi;
       if (lane == 0) {
         sh.digit = 64 * group + 63 - 2 * at - (low ? 1 : 0);
         sh.above = before + rest + (low ? first_hi : 0);
+        sh.equal = low ? first_lo : first_hi;
       }
     }
     __syncthreads();
@@ -289,50 +291,70 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const EvictArgs 
 
   // A warp takes neighbouring rows, so that ranks follow from ballots; four times 32 at once.
   constexpr int kUnroll = 4;
-  const int seg = (per + kWarps - 1) / kWarps, w0 = min(end, begin + warp * seg), w1 = min(end, w0 + seg);
+  const int seg = ((per + kWarps - 1) / kWarps + 31) / 32 * 32, w0 = min(end, begin + warp * seg), w1 = min(end, w0 + seg);
   const uint32_t lower = (1u << lane) - 1u;
   int eq_before = 0, none = 0, all = 0;
-  for (int i = w0; i < w1; i += 32 * kUnroll) {
-    uint32_t u[kUnroll];
+  const bool some_equal = need < sh.equal;       // not all rows of the last key that stays do: the first ones
+  if (some_equal) {
+    for (int i = w0; i < w1; i += 32 * kUnroll) {
+      uint32_t u[kUnroll];
 #pragma unroll
-    for (int j = 0; j < kUnroll; ++j) u[j] = i + 32 * j + lane < w1 ? key(i + 32 * j + lane) : ~prefix;
+      for (int j = 0; j < kUnroll; ++j) u[j] = i + 32 * j + lane < w1 ? key(i + 32 * j + lane) : ~prefix;
 #pragma unroll
-    for (int j = 0; j < kUnroll; ++j) eq_before += __popc(__ballot_sync(0xffffffffu, u[j] == prefix));
+      for (int j = 0; j < kUnroll; ++j) eq_before += __popc(__ballot_sync(0xffffffffu, u[j] == prefix));
+    }
+    sums_before(cluster, sh, 1, C, c, eq_before, none, all);
   }
-  sums_before(cluster, sh, 1, C, c, eq_before, none, all);
-  // every row of the warp's: whether it is a hole or moves
+  // every row of the warp's, 32 at a time: which are holes, which move
   auto walk = [&](auto&& each) {
     int equal = eq_before;
     for (int i = w0; i < w1; i += 32 * kUnroll) {
-      uint32_t u[kUnroll], same[kUnroll], hole[kUnroll], mover[kUnroll];
-      bool kept[kUnroll];
+      uint32_t u[kUnroll], hole[kUnroll], mover[kUnroll];
 #pragma unroll
       for (int j = 0; j < kUnroll; ++j) u[j] = i + 32 * j + lane < w1 ? key(i + 32 * j + lane) : 0u;
-#pragma unroll
-      for (int j = 0; j < kUnroll; ++j) same[j] = __ballot_sync(0xffffffffu, i + 32 * j + lane < w1 && u[j] == prefix);
 #pragma unroll
       for (int j = 0; j < kUnroll; ++j) {
         const int row = i + 32 * j + lane;
         const bool held = row < w1;
-        kept[j] = held && (u[j] > prefix || (u[j] == prefix && equal + __popc(same[j] & lower) < need));
-        equal += __popc(same[j]);
-        hole[j] = __ballot_sync(0xffffffffu, held && !kept[j] && row < k);
-        mover[j] = __ballot_sync(0xffffffffu, kept[j] && row >= k);
+        bool kept = held && u[j] >= prefix;
+        if (some_equal) {
+          const uint32_t same = __ballot_sync(0xffffffffu, held && u[j] == prefix);
+          kept = held && (u[j] > prefix || (u[j] == prefix && equal + __popc(same & lower) < need));
+          equal += __popc(same);
+        }
+        hole[j] = __ballot_sync(0xffffffffu, held && !kept && row < k);
+        mover[j] = __ballot_sync(0xffffffffu, kept && row >= k);
       }
 #pragma unroll
-      for (int j = 0; j < kUnroll; ++j) each(i + 32 * j + lane, hole[j], mover[j], kept[j]);
+      for (int j = 0; j < kUnroll; ++j) each(i + 32 * j, hole[j], mover[j]);
     }
   };
+  // What the first walk finds is kept for the second, in the place of the first histogram, which nobody reads any more.
+  uint32_t *const hole_bits = sh.hist[0] + warp * (seg / 32), *const mover_bits = hole_bits + kBins / 2;
+  const bool noted = kWarps * (seg / 32) <= kBins / 2;
   int at_hole = 0, at_mover = 0;
-  walk([&](int, uint32_t hole, uint32_t mover, bool) { at_hole += __popc(hole); at_mover += __popc(mover); });
-  sums_before(cluster, sh, 2, C, c, at_hole, at_mover, all);
-  walk([&](int row, uint32_t hole, uint32_t mover, bool kept) {
-    if (hole >> lane & 1) holes[at_hole + __popc(hole & lower)] = row;
-    if (mover >> lane & 1) movers[at_mover + __popc(mover & lower)] = row;
-    if (!E.in_place && kept && row < k) source[row] = row;
+  walk([&](int row, uint32_t hole, uint32_t mover) {
     at_hole += __popc(hole);
     at_mover += __popc(mover);
+    if (noted && lane == 0 && row < w1) {
+      hole_bits[(row - w0) / 32] = hole;
+      mover_bits[(row - w0) / 32] = mover;
+    }
   });
+  sums_before(cluster, sh, 2, C, c, at_hole, at_mover, all);
+  auto put = [&](int first_row, uint32_t hole, uint32_t mover) {
+    const int row = first_row + lane;
+    if (hole >> lane & 1) holes[at_hole + __popc(hole & lower)] = row;
+    else if (!E.in_place && row < min(w1, k)) source[row] = row;
+    if (mover >> lane & 1) movers[at_mover + __popc(mover & lower)] = row;
+    at_hole += __popc(hole);
+    at_mover += __popc(mover);
+  };
+  if (noted) {
+    for (int i = w0; i < w1; i += 32) put(i, hole_bits[(i - w0) / 32], mover_bits[(i - w0) / 32]);
+  } else {
+    walk(put);
+  }
   if (c == 0 && tid == 0) {
     E.n_moves[s] = all;
     if (E.lens_out) E.lens_out[s] = k;
@@ -426,9 +448,10 @@ cudaError_t launch_evict(const EvictArgs& E, cudaStream_t st) {
   attrs[1].val.clusterDim.y = attrs[1].val.clusterDim.z = 1;
   pc.cfg.attrs = attrs;
   pc.cfg.numAttrs = 2;
-  static std::atomic<unsigned long long> devices[2];
-  auto kern = fused ? evict_select_kernel<true> : evict_select_kernel<false>;
-  cudaError_t e = kernel_limits(kern, kStageRows * 8, devices[fused]);
+  static std::atomic<unsigned long long> devices[3];
+  const bool crowded = !fused && (int64_t)C * E.n_streams > 2 * kAttnSms;
+  auto kern = fused ? evict_select_kernel<true, 0> : crowded ? evict_select_kernel<false, 3> : evict_select_kernel<false, 0>;
+  cudaError_t e = kernel_limits(kern, kStageRows * 8, devices[fused ? 0 : crowded ? 1 : 2]);
   if (e == cudaSuccess) e = cudaLaunchKernelEx(&pc.cfg, kern, E, per, staged);
   if (e != cudaSuccess || fused || (E.in_place && E.list == 0)) return e;
   switch (E.row_bytes / 16) {
