@@ -486,6 +486,71 @@ def test_on_a_stream_of_its_own(cuda_lib, raw):
         assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_calls_that_overlap(cuda_lib, dtype):
+    """Two streams whose calls run at once, eagerly and as two captured graphs: each has workspaces of its own."""
+    inputs = [_inputs(3, dtype), _inputs(40, dtype)]
+    inputs[1]["lens"] = _lens([17, 400, 0])
+    want = [[y.clone() for y in _pass(cuda_lib, x)] for x in inputs]
+    sides = [torch.cuda.Stream() for _ in inputs]
+    torch.cuda.synchronize()
+    got = [None, None]
+    for _ in range(20):
+        for i in (0, 1):
+            got[i] = _pass(cuda_lib, inputs[i], stream=sides[i])
+    torch.cuda.synchronize()
+    for g, w in zip(got, want):
+        assert all(torch.equal(x, y) for x, y in zip(g, w))
+    graphs, held = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()], []
+    for graph, x in zip(graphs, inputs):
+        with torch.cuda.graph(graph):
+            held.append(_pass(cuda_lib, x))
+    for _ in range(20):
+        for i in (0, 1):
+            with torch.cuda.stream(sides[i]):
+                graphs[i].replay()
+    torch.cuda.synchronize()
+    for g, w in zip(held, want):
+        assert all(torch.equal(x, y) for x, y in zip(g, w))
+
+
+@pytest.mark.parametrize("dtype,B,cap", [("bf16", 40, 700), ("fp32", 40, 700), ("bf16", 2, 300), ("fp32", 2, 300)])
+def test_steps_without_waiting(cuda_lib, dtype, B, cap):
+    """A serving loop that never waits: what a step writes (rows, lens, queries, scores) is what the next one's launches see, early as they
+    begin.  The same steps with a wait behind every call give the same bits."""
+    t, H, g, d = TYPES[dtype], 8, 4, 128
+    S = B * H
+    pk, pv = _keys(1, H, 500, d, dtype=t), _normal(2, H, 500, d, dtype=t)
+    rows, queries = _keys(3, 25, S, d, dtype=t), _normal(4, 25, S, g, d, dtype=t)
+
+    def steps(wait):
+        k, v = _keys(5, S, cap, d, dtype=t), _normal(6, S, cap, d, dtype=t)
+        score, lens = torch.zeros(S, cap, device="cuda"), _lens([cap - 20 - 7 * (s % 9) for s in range(S)])
+        pos, q, results = torch.arange(cap, dtype=torch.int32, device="cuda").repeat(S, 1), torch.empty(S, g, d, dtype=t, device="cuda"), []
+        at = torch.arange(S, device="cuda")
+        for i in range(25):
+            k[at, lens.long()] = rows[i]
+            v[at, lens.long()] = rows[i].flip(-1)
+            score[at, lens.long()] = 0
+            pos[at, lens.long()] = cap + i
+            lens += 1
+            q.copy_(queries[i])
+            out, _ = cuda_lib.attn_scored(k, v, q, lens=lens, score=score, decay=0.9)
+            if wait:
+                torch.cuda.synchronize()
+            cuda_lib.cache_evict(k, v, score, cap - 15, lens=lens, pos=pos, n_first=4, n_recent=20, in_place=True)
+            if wait:
+                torch.cuda.synchronize()
+            ahead = cuda_lib.decode_attn_prefix(pk, pv, k.view(B, H, cap, d), v.view(B, H, cap, d), q.view(B, H * g, d), lens=lens[::H].contiguous())
+            if wait:
+                torch.cuda.synchronize()
+            results += [out, ahead]
+        return [*results, k, v, score, lens, pos]
+
+    for a, b in zip(steps(True), steps(False)):
+        assert torch.equal(a, b)
+
+
 def test_refusals_with_a_device(cuda_lib):
     k, q, score = torch.zeros(2, 10, 64, device="cuda"), torch.zeros(2, 3, 64, device="cuda"), torch.zeros(2, 10, device="cuda")
     bk = cuda_lib
