@@ -48,6 +48,10 @@ struct Few {
 // Warps of a CTA of attn_few_kernel, so that two share an SM and one starts or ends while the other reads (fp32 rows of 128 dims, 1024 streams of up
 // to 512 rows: 85 us by four warps, 77 by two; 2048 of 64, five query rows: 188 and 124).
 __host__ __device__ constexpr int few_warps(bool bf16, int d) { return !bf16 && d == 128 ? 2 : kWarps; }
+// Launches of more than two waves take less from a ring that stays full than from another CTA that is in the middle of its tiles while two start or
+// end: bf16 rows of 128 dims, 256 streams of up to 8192 rows, 1792 CTAs: 96.3 us by two an SM, 94.5 by three; 2048 CTAs of 128 rows 41.4
+// and 37.3; 296 of 512 rows 10.5 and 13.9.
+__host__ __device__ constexpr bool few_crowded(bool bf16, int d, int64_t ctas) { return bf16 && d == 128 && ctas > 4 * kAttnSms; }
 
 struct FewArgs {
   AttnRows A;
@@ -78,7 +82,7 @@ struct Logits {
 
 // This warp's tiles of the CTA's share: every W-th (a warp of the CTA each) of [t0, t1) from t0 + warp on.  Tile number n of the warp has the ring's
 // entries 2 n (K) and 2 n + 1 (V).
-template <bool kBf16, int D, int W>
+template <bool kBf16, int D, int W, int N>
 struct Ring {
   using F = Few<kBf16, D>;
   const CUtensorMap *mk, *mv;
@@ -89,34 +93,34 @@ struct Ring {
 
   __device__ void issue(int e) const {           // one lane
     const CUtensorMap* map = e & 1 ? mv : mk;
-    const int s = e % F::kRing, row = (first_tile + (e >> 1) * W) * kTile;
+    const int s = e % N, row = (first_tile + (e >> 1) * W) * kTile;
     tc::mbar_expect_tx(full + s, F::kTileBytes);
 #pragma unroll
     for (int b = 0; b < F::kBoxes; ++b) tma_load_3d(tiles + s * F::kTileBytes + b * kBox, map, b * F::kBoxDims, row, stream, full + s, policy);
   }
   __device__ void start(int lane) const {
     if (lane == 0)
-      for (int e = 0; e < min(F::kRing, entries); ++e) issue(e);
+      for (int e = 0; e < min(N, entries); ++e) issue(e);
   }
   __device__ bool wait(int e, int lane, int* abort_flag) const {
     bool ok = true;
-    if (lane == 0) ok = tc::wait_bar(full + e % F::kRing, (uint32_t)(e / F::kRing) & 1u, abort_flag);
+    if (lane == 0) ok = tc::wait_bar(full + e % N, (uint32_t)(e / N) & 1u, abort_flag);
     ok = __shfl_sync(0xffffffffu, ok, 0);
     __syncwarp();
     return ok;
   }
   __device__ void next(int e, int lane) const {  // entry e has been read by the whole warp
     __syncwarp();
-    if (lane == 0 && e + F::kRing < entries) issue(e + F::kRing);
+    if (lane == 0 && e + N < entries) issue(e + N);
   }
   // A wait gave up: the copies behind entry e that have been asked for are waited for, within limits, before the ring is left.
   __device__ void drain(int e, int lane) const {
     if (lane != 0) return;
     const long long t0 = clock64();
-    for (int i = e; i < min(e + F::kRing, entries); ++i)
-      while (!tc::mbar_try_wait(full + i % F::kRing, (uint32_t)(i / F::kRing) & 1u) && clock64() - t0 < tc::kWaitCycles) {}
+    for (int i = e; i < min(e + N, entries); ++i)
+      while (!tc::mbar_try_wait(full + i % N, (uint32_t)(i / N) & 1u) && clock64() - t0 < tc::kWaitCycles) {}
   }
-  __device__ const unsigned char* at(int e) const { return tiles + e % F::kRing * F::kTileBytes; }
+  __device__ const unsigned char* at(int e) const { return tiles + e % N * F::kTileBytes; }
 };
 
 // Byte offset of 16-byte piece p of a row.
@@ -140,8 +144,8 @@ struct TileWeights {
 };
 
 // The warp's sums of its tiles, to mrg[row][kPitch].
-template <int D, int W>
-__device__ inline void few_warp_bf16(const AttnRows& A, const Group& G, const Logits& X, const Ring<true, D, W>& R, int s, int len, int n_tiles, int lane, int* abort_flag,
+template <int D, int W, int N>
+__device__ inline void few_warp_bf16(const AttnRows& A, const Group& G, const Logits& X, const Ring<true, D, W, N>& R, int s, int len, int n_tiles, int lane, int* abort_flag,
                                      float* mrg, bool& failed) {
   const int g = G.g;
   // With up to four rows the columns 4-7 repeat the rows 0-3, and in the second product they carry the low parts of the weights:
@@ -293,8 +297,8 @@ __device__ inline void few_warp_bf16(const AttnRows& A, const Group& G, const Lo
 // sets that take every kT-th row, each lane a part of the columns.  (A lane per row with the queries read from shared memory, and all
 // lanes on every row of V: 4300 cycles a tile of d = 64 and four queries.)
 // qs: [kR][D]; ps: [kR][32] of this warp.
-template <int D, int kR, int W>
-__device__ inline void few_warp_fp32(const AttnRows& A, const Group& G, const Logits& X, const Ring<false, D, W>& R, int s, int len, int n_tiles, int lane, int* abort_flag,
+template <int D, int kR, int W, int N>
+__device__ inline void few_warp_fp32(const AttnRows& A, const Group& G, const Logits& X, const Ring<false, D, W, N>& R, int s, int len, int n_tiles, int lane, int* abort_flag,
                                      const float* qs, float* ps, float* mrg, bool& failed) {
   const int g = G.g;
   constexpr int kAtOnce = kR < 4 ? kR : 4;       // queries whose logits are formed together; of more, they come from shared memory for each tile
@@ -435,22 +439,22 @@ __device__ inline void few_warp_fp32(const AttnRows& A, const Group& G, const Lo
 }
 
 // What a CTA needs in shared memory besides the rings.
-template <bool kBf16, int D, int kR, int W>
+template <bool kBf16, int D, int kR, int W, int N>
 struct FewShared {
-  uint64_t full[W][Few<kBf16, D>::kRing];
+  uint64_t full[W][N];
   int abort_flag;
   __align__(16) float qs[kBf16 ? 4 : kR * D];
   __align__(16) float ps[kBf16 ? 4 : W * kR * 32];
 };
 
 // The CTA's share [t0, t1) of the tiles: every warp's sums, to mrg[warp][row][kPitch] in the rings' place.
-template <bool kBf16, int D, int kR, int W>
-__device__ inline void few_tiles(const AttnRows& A, const Group& G, const Logits& X, const CUtensorMap& mk, const CUtensorMap& mv, FewShared<kBf16, D, kR, W>& sh, unsigned char* tiles,
+template <bool kBf16, int D, int kR, int W, int N>
+__device__ inline void few_tiles(const AttnRows& A, const Group& G, const Logits& X, const CUtensorMap& mk, const CUtensorMap& mv, FewShared<kBf16, D, kR, W, N>& sh, unsigned char* tiles,
                                  int s, int len, int t0, int t1, bool leaving) {
   using F = Few<kBf16, D>;
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
   const int n_tiles = max(0, (t1 - t0 - warp + W - 1) / W);
-  const Ring<kBf16, D, W> R{&mk, &mv, tiles + warp * F::kRing * F::kTileBytes, sh.full[warp], s, t0 + warp, 2 * n_tiles, l2_policy(leaving)};
+  const Ring<kBf16, D, W, N> R{&mk, &mv, tiles + warp * N * F::kTileBytes, sh.full[warp], s, t0 + warp, 2 * n_tiles, l2_policy(leaving)};
   R.start(lane);
   if constexpr (!kBf16) {
     for (int i = tid; i < kR * D; i += 32 * W)
@@ -459,18 +463,18 @@ __device__ inline void few_tiles(const AttnRows& A, const Group& G, const Logits
   }
   float* mrg = reinterpret_cast<float*>(tiles) + warp * kFewRows * F::kPitch;
   bool failed = false;
-  if constexpr (kBf16) few_warp_bf16<D, W>(A, G, X, R, s, len, n_tiles, lane, &sh.abort_flag, mrg, failed);
-  else few_warp_fp32<D, kR, W>(A, G, X, R, s, len, n_tiles, lane, &sh.abort_flag, sh.qs, sh.ps + warp * kR * 32, mrg, failed);
+  if constexpr (kBf16) few_warp_bf16<D, W, N>(A, G, X, R, s, len, n_tiles, lane, &sh.abort_flag, mrg, failed);
+  else few_warp_fp32<D, kR, W, N>(A, G, X, R, s, len, n_tiles, lane, &sh.abort_flag, sh.qs, sh.ps + warp * kR * 32, mrg, failed);
   if (failed && lane == 0) tc::st_release(&sh.abort_flag, 1);
   __syncthreads();
 }
 
-template <bool kBf16, int D, int kR, int W>
-__device__ inline void few_init(FewShared<kBf16, D, kR, W>& sh, const CUtensorMap& mk, const CUtensorMap& mv) {
+template <bool kBf16, int D, int kR, int W, int N>
+__device__ inline void few_init(FewShared<kBf16, D, kR, W, N>& sh, const CUtensorMap& mk, const CUtensorMap& mv) {
   if (threadIdx.x != 0) return;
   asm volatile("prefetch.tensormap [%0];" ::"l"(&mk) : "memory");
   asm volatile("prefetch.tensormap [%0];" ::"l"(&mv) : "memory");
-  for (int i = 0; i < W * Few<kBf16, D>::kRing; ++i) tc::mbar_init(&sh.full[0][0] + i, 1);
+  for (int i = 0; i < W * N; ++i) tc::mbar_init(&sh.full[0][0] + i, 1);
   sh.abort_flag = 0;
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -569,13 +573,13 @@ __device__ inline void join_before(const AttnRows& A, int64_t row, int lane, flo
     }
 }
 
-// kR: rows that the fp32 form takes (bf16: 8).
-template <bool kBf16, int D, int kR>
-__global__ void __launch_bounds__(32 * few_warps(kBf16, D), 2) attn_few_kernel(const __grid_constant__ FewJobs J, const __grid_constant__ FewMaps maps) {
+// kR: rows that the fp32 form takes (bf16: 8).  kCtas share an SM; three, with rings of two tiles (few_crowded).
+template <bool kBf16, int D, int kR, int kCtas>
+__global__ void __launch_bounds__(32 * few_warps(kBf16, D), kCtas) attn_few_kernel(const __grid_constant__ FewJobs J, const __grid_constant__ FewMaps maps) {
   using F = Few<kBf16, D>;
-  constexpr int W = few_warps(kBf16, D);
+  constexpr int W = few_warps(kBf16, D), N = kCtas == 3 ? 2 : F::kRing;
   extern __shared__ unsigned char smem_raw[];
-  __shared__ FewShared<kBf16, D, kR, W> sh;
+  __shared__ FewShared<kBf16, D, kR, W, N> sh;
   unsigned char* tiles = smem_raw + (-tc::smem_u32(smem_raw) & 1023u);
   const int which = (int)blockIdx.x >= J.ctas0, cta = blockIdx.x - (which ? J.ctas0 : 0);
   const AttnRows& A = J.job[which].A;
@@ -639,7 +643,7 @@ attn_few_cluster_kernel(const __grid_constant__ AttnRows A, const ScoreArgs S, i
   namespace cg = cooperative_groups;
   using F = Few<kBf16, D>;
   extern __shared__ unsigned char smem_raw[];
-  __shared__ FewShared<kBf16, D, kR, kWarps> sh;
+  __shared__ FewShared<kBf16, D, kR, kWarps, F::kRing> sh;
   __shared__ float lse[kFewRows];
   unsigned char* tiles = smem_raw + (-tc::smem_u32(smem_raw) & 1023u);
   float* x = reinterpret_cast<float*>(tiles + kWarps * F::kRing * F::kTileBytes);      // [g][pitch]
@@ -826,14 +830,19 @@ cudaError_t launch_few(const FewArgs& P, const FewArgs* also, FewOrder order, cu
   }
   if (ctas > INT32_MAX) return cudaErrorInvalidValue;
   return for_rows<kBf16, group_rows(kBf16, D)>(most, [&](auto rows) {
-    auto kern = attn_few_kernel<kBf16, D, decltype(rows)::value>;
-    static std::atomic<unsigned long long> devices{0};
-    constexpr int W = few_warps(kBf16, D);
-    constexpr size_t smem = 1024 + (size_t)W * F::kRing * F::kTileBytes;
-    const cudaError_t e = kernel_limits(kern, smem, devices);
-    if (e != cudaSuccess) return e;
-    const PdlConfig pc(dim3((unsigned)ctas), 32 * W, smem, st);
-    return cudaLaunchKernelEx(&pc.cfg, kern, J, maps);
+    auto run = [&](auto kern, int ring, std::atomic<unsigned long long>& devices) {
+      constexpr int W = few_warps(kBf16, D);
+      const size_t smem = 1024 + (size_t)W * ring * F::kTileBytes;
+      const cudaError_t e = kernel_limits(kern, smem, devices);
+      if (e != cudaSuccess) return e;
+      const PdlConfig pc(dim3((unsigned)ctas), 32 * W, smem, st);
+      return cudaLaunchKernelEx(&pc.cfg, kern, J, maps);
+    };
+    constexpr int kR = decltype(rows)::value;
+    static std::atomic<unsigned long long> devices[2];
+    if constexpr (few_crowded(kBf16, D, INT64_MAX))
+      if (few_crowded(kBf16, D, ctas)) return run(attn_few_kernel<kBf16, D, kR, 3>, 2, devices[1]);
+    return run(attn_few_kernel<kBf16, D, kR, 2>, F::kRing, devices[0]);
   });
 }
 
