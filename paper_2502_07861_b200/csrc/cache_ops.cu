@@ -89,19 +89,21 @@ bool prefix_by_few(const AttnRows& P, int dtype) { return P.n_rows <= (dtype ? k
 
 // Whether the sequences' own rows are read beside the tensor-core kernel's work on the prefix, which then leaves them SMs, and by how many splits
 // that works.  Times in us: a pair of query tiles with a tile of keys takes 1.7, a tile of keys by itself 1.55 (it waits for memory); the one-pass
-// kernel reads 6 MB and a wave of its CTAs takes 4.5.  The SMs are shared out by these times, the tensor-core kernel's counted half as long again,
-// since others now read too.  It costs a launch that joins, unless the own rows need one anyway: short ones finish the outputs themselves instead
-// (64 x 4 x 8 behind 32768 rows, 200 own: 52 us against 55), and where the tensor-core kernel waits for memory too, so do all that are not most of the
-// work.  (256 sequences x 5 heads x 8 behind 8192 rows: with 1024 own rows each 210 us one after the other, 192 so, 256 own rows
-// 116 and 103; 128 x 8 x 4 behind 16384, 300 own: 61 and 54; 32 x 4 x 8 behind 32768, 512 own: 44 and 48, 2048 own: 83 and 77.)
+// kernel reads 6 MB and a wave of its CTAs takes 4.5.  The SMs are shared out by these times, the tensor-core kernel's counted half as long
+// again, since others now read too, the own rows' at half of their capacity, which is what they fill on the way; three quarters at most (128 x 8 x 4
+// behind 16384 rows, 300 own each: 55 us by 112 CTAs, 69 by 128).  256 sequences x 5 heads x 8 behind 8192 rows: with 1024 own rows each
+// 210 us one after the other, 192 so, with up to 1024 146 and 129, with 256 116 and 91.
+// It costs a launch that joins, unless the own rows need one anyway: short ones finish the outputs themselves instead (64 x 4 x 8 behind 32768
+// rows, 200 own: 52 us against 55), and where the tensor-core kernel waits for memory too, so do all that are not most of the work (32 x 4 x 8
+// behind 32768, 512 own: 44 and 48; 2048 own: 83 and 74).
 bool prefix_beside(const AttnRows& P, const AttnRows& A, int head_dim, int& splits) {
   const bool by_keys = attn_tc_by_keys(P);
   const int64_t blocks = attn_tc_blocks(P), tiles = (P.cap + 127) / 128;
   const double prefix = (double)blocks * tiles * (by_keys ? 1.55 : 1.7) / kAttnSms;
   const int64_t waves = ((int64_t)A.n_streams * A.splits + 2 * kAttnSms - 1) / (2 * kAttnSms);
-  const double own = std::max((double)A.n_streams * A.cap * head_dim * 4 / 6e6, 4.5 * waves);
+  const double bytes = (double)A.n_streams * A.cap * head_dim * 4, own = std::max(bytes / 6e6, 4.5 * waves), usual = std::max(bytes / 12e6, 4.5 * waves);
   if (A.splits == 1 && (own < 10 || (by_keys && own < 1.5 * prefix))) return false;
-  const double sms = kAttnSms * 1.5 * prefix / (1.5 * prefix + own);
+  const double sms = kAttnSms * std::min(0.75, 1.5 * prefix / (1.5 * prefix + usual));
   splits = (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)std::ceil(sms / blocks), tiles / 2, kAttnMaxSplits}));
   return true;
 }
