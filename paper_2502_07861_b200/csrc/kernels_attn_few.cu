@@ -48,10 +48,13 @@ struct Few {
 // Warps of a CTA of attn_few_kernel, so that two share an SM and one starts or ends while the other reads (fp32 rows of 128 dims, 1024 streams of up
 // to 512 rows: 85 us by four warps, 77 by two; 2048 of 64, five query rows: 188 and 124).
 __host__ __device__ constexpr int few_warps(bool bf16, int d) { return !bf16 && d == 128 ? 2 : kWarps; }
-// Launches of more than two waves take less from a ring that stays full than from another CTA that is in the middle of its tiles while two start or
-// end: bf16 rows of 128 dims, 256 streams of up to 8192 rows, 1792 CTAs: 96.3 us by two an SM, 94.5 by three; 2048 CTAs of 128 rows 41.4
-// and 37.3; 296 of 512 rows 10.5 and 13.9.
-__host__ __device__ constexpr bool few_crowded(bool bf16, int d, int64_t ctas) { return bf16 && d == 128 && ctas > 4 * kAttnSms; }
+// Launches of more than two waves take less from a ring that stays full than from another CTA that is in the middle of its tiles while others start or
+// end: three CTAs an SM with rings of two tiles, of 64 dims four with three.  bf16 rows, five query rows, two CTAs an SM and so: 256 streams of
+// up to 8192 rows of 128 dims 96.3 and 94.5 us, 2048 of 128 rows 41.4 and 37.3, 296 of 512 (one wave) 10.5 and 13.9; of 64 dims 57.2 and
+// 50.4, 29.7 and 21.5.
+__host__ __device__ constexpr bool few_crowded(bool bf16, int64_t ctas) { return bf16 && ctas > 4 * kAttnSms; }
+__host__ __device__ constexpr int crowd_ctas(int d) { return d == 128 ? 3 : 4; }
+__host__ __device__ constexpr int crowd_ring(int d) { return d == 128 ? 2 : 3; }
 
 struct FewArgs {
   AttnRows A;
@@ -573,11 +576,11 @@ __device__ inline void join_before(const AttnRows& A, int64_t row, int lane, flo
     }
 }
 
-// kR: rows that the fp32 form takes (bf16: 8).  kCtas share an SM; three, with rings of two tiles (few_crowded).
+// kR: rows that the fp32 form takes (bf16: 8).  kCtas share an SM (more than two: few_crowded).
 template <bool kBf16, int D, int kR, int kCtas>
 __global__ void __launch_bounds__(32 * few_warps(kBf16, D), kCtas) attn_few_kernel(const __grid_constant__ FewJobs J, const __grid_constant__ FewMaps maps) {
   using F = Few<kBf16, D>;
-  constexpr int W = few_warps(kBf16, D), N = kCtas == 3 ? 2 : F::kRing;
+  constexpr int W = few_warps(kBf16, D), N = kCtas == 2 ? F::kRing : crowd_ring(D);
   extern __shared__ unsigned char smem_raw[];
   __shared__ FewShared<kBf16, D, kR, W, N> sh;
   unsigned char* tiles = smem_raw + (-tc::smem_u32(smem_raw) & 1023u);
@@ -840,8 +843,8 @@ cudaError_t launch_few(const FewArgs& P, const FewArgs* also, FewOrder order, cu
     };
     constexpr int kR = decltype(rows)::value;
     static std::atomic<unsigned long long> devices[2];
-    if constexpr (few_crowded(kBf16, D, INT64_MAX))
-      if (few_crowded(kBf16, D, ctas)) return run(attn_few_kernel<kBf16, D, kR, 3>, 2, devices[1]);
+    if constexpr (kBf16)
+      if (few_crowded(kBf16, ctas)) return run(attn_few_kernel<kBf16, D, kR, crowd_ctas(D)>, crowd_ring(D), devices[1]);
     return run(attn_few_kernel<kBf16, D, kR, 2>, F::kRing, devices[0]);
   });
 }
