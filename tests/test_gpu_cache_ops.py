@@ -333,6 +333,38 @@ def test_own_rows_beside_the_prefix(cuda_lib, d, B, H, g, P, cap, weighted):
         _check_prefix(cuda_lib, "bf16", d, B, H, g, P, cap, [(31 * b * (call + 1)) % (cap + 1) for b in range(B)], weighted, seed=B + call)
 
 
+def test_own_rows_beside_the_prefix_captured(cuda_lib):
+    """The same in a graph, several calls in a row, replayed on other queries, rows and lengths than were captured."""
+    B, H, g, P, cap, d = 200, 4, 3, 3000, 400, 128
+    t = torch.bfloat16
+
+    def inputs(seed):
+        return [_keys(seed, H, P, d, dtype=t), _normal(seed + 1, H, P, d, dtype=t), _keys(seed + 2, B, H, cap, d, dtype=t), _normal(seed + 3, B, H, cap, d, dtype=t),
+                _normal(seed + 4, B, H * g, d, dtype=t), _lens([(seed + 29 * b) % (cap + 1) for b in range(B)])]
+
+    def calls(x):
+        first = cuda_lib.decode_attn_prefix(*x[:5], lens=x[5])
+        second = cuda_lib.decode_attn_prefix(*x[:4], first, lens=x[5])         # its queries are what the first call wrote
+        return [first, second, cuda_lib.decode_attn_prefix(*x[:4], second, lens=x[5])]
+
+    a, b = inputs(1), inputs(50)
+    want = [[y.clone() for y in calls(x)] for x in (a, b)]
+    torch.cuda.synchronize()
+    held, graph = [x.clone() for x in a], torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = calls(held)
+    for source, w in ((b, want[1]), (a, want[0]), (b, want[1])):
+        for x, y in zip(held, source):
+            x.copy_(y)
+        for _ in range(3):
+            graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(got, w))
+    for _ in range(10):
+        again = calls(a)
+    assert all(torch.equal(x, y) for x, y in zip(again, want[0]))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("B", [1, 40, 200])
 def test_prefix_whose_rows_are_all_absent(cuda_lib, dtype, B):
