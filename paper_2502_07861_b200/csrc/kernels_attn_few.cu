@@ -890,7 +890,7 @@ cudaError_t launch_end(const FewArgs& P, const ScoreArgs& S, cudaStream_t st) {
 }  // namespace
 
 // Split factor of the kernels above: as many CTAs as fit the SMs at once, with a tile for each warp; and of long caches, in parts of 1024
-// rows, up to six times as many, so that streams of different lengths even out (256 streams of up to 8192 rows: 104.9 us by 5 splits, 102.2 by 7).
+// rows, up to six times as many, so that streams of different lengths even out (256 streams of up to 8192 rows: 96.6 us by 5 splits, 93.8 by 7).
 int few_splits(int64_t streams, int cap, int n_rows, int d, int is_bf16) {
   const int64_t sets = streams * ((n_rows + group_rows(is_bf16, d) - 1) / group_rows(is_bf16, d));
   const int share = few_warps(is_bf16, d) * kTile;
