@@ -83,7 +83,7 @@ int plan_scored(AttnRows& A, float*& x, Pieces& ws, int n_streams, int capacity,
 
 // ---- decode_attn_prefix
 
-// Whether the one-pass kernels take the prefix, eight query rows to a CTA: fp32 has no tensor cores to go to, and its tiles of 64 query
+// Whether the one-pass kernels take the prefix, eight query rows to a CTA: fp32 has no tensor cores to go to, and its tiles of 128 query
 // rows pay only when there are a few of them.
 bool prefix_by_few(const AttnRows& P, int dtype) { return P.n_rows <= (dtype ? kFewRows : 128); }
 
