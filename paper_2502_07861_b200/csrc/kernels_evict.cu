@@ -8,6 +8,7 @@
 #include <cooperative_groups.h>
 
 #include <algorithm>
+#include <utility>
 
 #include "attn_rows.cuh"
 
@@ -122,8 +123,11 @@ __global__ void __launch_bounds__(kThreads, kCtas) evict_select_kernel(const Evi
   const int C = (int)cluster.num_blocks(), c = (int)cluster.block_rank();
   const int s = blockIdx.x / C, tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
   for (int i = tid; i < kPasses * kBins / 4; i += kThreads) reinterpret_cast<uint4*>(&sh.hist[0][0])[i] = make_uint4(0, 0, 0, 0);
+  // Nobody counts rows before the histograms are empty, and nobody writes into another CTA's shared memory before that CTA has begun.
+  auto begun = cluster.barrier_arrive();
   grid_wait_and_release();
   const int len = E.lens ? max(0, min(E.lens[s], E.cap)) : E.cap, k = min(len, E.keep);
+  cluster.barrier_wait(std::move(begun));
   const int64_t first = (int64_t)s * E.cap;
   int* holes = E.moves + (int64_t)s * (2 * (int64_t)E.list + (E.in_place ? 0 : E.keep));
   int* movers = holes + E.list;
