@@ -93,6 +93,27 @@ __device__ inline float2 exp2_fma(float2 x) {
   return make_float2(__uint_as_float(__float_as_uint(p.x) + (__float_as_uint(t.x) << 23)), __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(t.y) << 23)));
 }
 
+// What a warp asked for or issued is over before its CTA uses the memory for something else or ends, whichever warp gave up and when: the last warp
+// to leave waits for it, within limits.  (Without a wait that gave up, another warp has seen the same phases before.)  The copies of a ring, of which
+// `asked` entries have been asked for:
+template <int kRing>
+__device__ inline void copies_landed(uint64_t (&full)[kRing], int asked) {
+  const long long t0 = clock64();
+  for (int i = max(0, asked - kRing); i < asked; ++i)
+    while (!mbar_try_wait(full + i % kRing, (uint32_t)(i / kRing) & 1u) && clock64() - t0 < kWaitCycles) {}
+}
+// a copy by itself:
+__device__ inline void copy_landed(uint64_t* full) {
+  const long long t0 = clock64();
+  while (!mbar_try_wait(full, 0) && clock64() - t0 < kWaitCycles) {}
+}
+// and the products that this warp issued:
+__device__ inline void products_done(uint64_t* drained) {
+  if (elect_one()) umma_commit(drained);
+  __syncwarp();
+  copy_landed(drained);
+}
+
 template <int kRegs>
 __device__ inline void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegs)); }
 template <int kRegs>

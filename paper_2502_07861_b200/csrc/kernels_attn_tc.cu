@@ -173,11 +173,9 @@ attn_tc_kernel(const __grid_constant__ TcArgs P, const __grid_constant__ CUtenso
             read_ahead(j0 + n_bias);             // (K tiles are loaded in their order)
           }
         }
-      if (!ok && lane == 0) {                    // gave up: the copies in flight, within limits
-        const long long t0 = clock64();
-        while (!mbar_try_wait(&q_full, 0) && clock64() - t0 < kWaitCycles) {}
-        for (int i = max(0, e - kRing); i < e; ++i)
-          while (!mbar_try_wait(kv_full + i % kRing, (uint32_t)(i / kRing) & 1u) && clock64() - t0 < kWaitCycles) {}
+      if (lane == 0) {
+        copy_landed(&q_full);
+        copies_landed(kv_full, e);
       }
     } else if (warp == 9 && n > 0) {
       constexpr uint32_t kInstrPv = kInstrBf16<D> | kOuterB;
@@ -252,12 +250,8 @@ attn_tc_kernel(const __grid_constant__ TcArgs P, const __grid_constant__ CUtenso
           }
         }
       }
-      if (!ok) {                                 // gave up: the products in flight, within limits
-        if (elect_one()) umma_commit(&drained);
-        st_release(&abort_flag, 1);
-        const long long t0 = clock64();
-        while (!mbar_try_wait(&drained, 0) && clock64() - t0 < kWaitCycles) {}
-      }
+      if (!ok) st_release(&abort_flag, 1);
+      products_done(&drained);
     }
   } else {
     regs_up<kRegsRows>();
@@ -359,7 +353,10 @@ attn_tc_kernel(const __grid_constant__ TcArgs P, const __grid_constant__ CUtenso
       ok = __all_sync(0xffffffffu, wait_bar(o_done + t, (uint32_t)(mine - 1) & 1u, &abort_flag));
       tc_fence_after();
     }
-    if (!ok) l = NAN;
+    if (!ok) {
+      l = NAN;
+      copy_landed(&q_full);                      // (what follows takes the Q tiles' place)
+    }
     // The results leave by way of shared memory, 32 columns of a warp's rows at a time, so that neighbouring lanes write neighbouring bytes
     // (a row per lane, 16 bytes at a time, took 8200 cycles for two tiles of sums).  Its Q tile is there for it: every S is formed.
     uint4* const stage = reinterpret_cast<uint4*>(sm + t * Sh::kTile) + (warp % 4) * (Sh::kTile / 64);

@@ -122,11 +122,9 @@ score_tc_kernel(const __grid_constant__ AttnRows A, const ScoreArgs C, int box_r
         }
         __syncwarp();
       }
-      if (i < n && lane == 0) {                  // gave up: the copies in flight, within limits
-        const long long t0 = clock64();
-        while (!mbar_try_wait(&k_full, 0) && clock64() - t0 < kWaitCycles) {}
-        for (int e = max(0, i - kRing); e < i; ++e)
-          while (!mbar_try_wait(q_full + e % kRing, (uint32_t)(e / kRing) & 1u) && clock64() - t0 < kWaitCycles) {}
+      if (lane == 0) {
+        copy_landed(&k_full);
+        copies_landed(q_full, i);
       }
     } else if (warp == 17 && n > 0) {
       bool ok = true;
@@ -150,12 +148,8 @@ score_tc_kernel(const __grid_constant__ AttnRows A, const ScoreArgs C, int box_r
         }
         __syncwarp();
       }
-      if (!ok) {                                 // gave up: the products in flight, within limits
-        if (elect_one()) umma_commit(&drained);
-        st_release(&abort_flag, 1);
-        const long long t0 = clock64();
-        while (!mbar_try_wait(&drained, 0) && clock64() - t0 < kWaitCycles) {}
-      }
+      if (!ok) st_release(&abort_flag, 1);
+      products_done(&drained);
     }
   } else {
     regs_up<kRegsRows>();
@@ -354,11 +348,9 @@ score_stream_kernel(const __grid_constant__ AttnRows A, const ScoreArgs C, int b
       if (lane == 0) ask_keys(i);
       __syncwarp();
     }
-    if (i < n && lane == 0) {                    // gave up: the copies in flight, within limits
-      const long long w0 = clock64();
-      while (!mbar_try_wait(&q_full, 0) && clock64() - w0 < kWaitCycles) {}
-      for (int e = max(0, i - kRing); e < i; ++e)
-        while (!mbar_try_wait(k_full + e % kRing, (uint32_t)(e / kRing) & 1u) && clock64() - w0 < kWaitCycles) {}
+    if (lane == 0) {
+      copy_landed(&q_full);
+      copies_landed(k_full, i);
     }
   } else if (warp == 9 && n > 0) {
     bool ok = true;
@@ -384,12 +376,8 @@ score_stream_kernel(const __grid_constant__ AttnRows A, const ScoreArgs C, int b
         __syncwarp();
       }
     }
-    if (!ok) {                                   // gave up: the products in flight, within limits
-      if (elect_one()) umma_commit(&drained);
-      st_release(&abort_flag, 1);
-      const long long w0 = clock64();
-      while (!mbar_try_wait(&drained, 0) && clock64() - w0 < kWaitCycles) {}
-    }
+    if (!ok) st_release(&abort_flag, 1);
+    products_done(&drained);
   } else if (warp < 8) {
     const int h = warp / 4, lanes = 32 * (warp % 4);
     const uint32_t S = tmem + ((uint32_t)lanes << 16);
