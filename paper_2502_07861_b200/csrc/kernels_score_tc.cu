@@ -12,8 +12,10 @@
 // query's lse from shared memory, whose loads share a queue with the exponentials: 345 us for a prompt of 8192 queries and 32 heads, 321 so.)
 // Two pairs of warpgroups take tiles in turn, half of the cached rows each, from four buffers of 128 x 128 logits in TMEM.
 // Where there are few CTAs the tiles are shared out to a cluster, whose sums meet in shared memory.
-// What bounds it are the exponentials: 16384 per tile of queries are 1024 cycles of the special-function unit against 512 of products
-// (d = 128), so a share of them is formed by FMAs.
+// No pipe bounds it (40 streams of 8192 rows, 512 queries x 4 heads: exponentials take 52 % of theirs, products 32 %, instructions issue in half of
+// the cycles): the row warps wait for TMEM, of which one load of 8 columns is on its way; registers hold no more beside the sums.  A quarter
+// of the exponentials is formed by FMAs, which saves a little of the special-function unit's queue (a prompt of 8192 queries and 32 heads with its
+// attention: 866 us so, 874 without).
 // Warps: 0-7 and 8-15 the queries of even and odd tiles, 16 asks for K and the Q tiles (TMA), 17 issues the MMAs.
 // Every wait is bounded; one that gives up makes the scores NaN.
 #include <cooperative_groups.h>
@@ -223,8 +225,9 @@ score_tc_kernel(const __grid_constant__ AttnRows A, const ScoreArgs C, int box_r
           }
         }
       };
-      // masked: some query does not see all of the rows, or a lane has no query that counts, whatever it holds
-      if (__any_sync(0xffffffffu, sees < kMine || off == -INFINITY)) weights(std::true_type{});
+      // masked: some query does not see all of the rows, or a lane has no query that counts, whatever it holds; or its lse is not a number, which
+      // exp2_fma would make one
+      if (__any_sync(0xffffffffu, sees < kMine || !(off > -INFINITY))) weights(std::true_type{});
       else weights(std::false_type{});
     }
     // over the warp's queries: 32 of the rows at a time, row `lane` of them to a lane

@@ -1,8 +1,12 @@
-"""Operators on caller-held caches, at edges of their own: selections whose clusters meet nowhere before the first count."""
+"""Operators on caller-held caches, at edges of their own: selections whose clusters meet nowhere before the first count, queries that are not
+numbers."""
+import math
+
 import pytest
 import torch
 
-from test_gpu_cache_ops import _check_evict, _lens, _normal
+from cache_ops_util import scored
+from test_gpu_cache_ops import TYPES, _check_evict, _keys, _lens, _near, _normal
 
 pytestmark = pytest.mark.gpu
 
@@ -33,3 +37,32 @@ def test_eviction_call_after_call_beside_other_work(cuda_lib, n_recent):
         got = cuda_lib.cache_evict(k, v, score, 4000, lens=lens, n_recent=n_recent)
         assert all(torch.equal(got[name], want[name]) for name in want)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("d,g,cap,m,n_scored,bad", [
+    (128, 4, 1000, 1, 1, 0), (64, 8, 9000, 1, 1, 0),                                        # one pass: clusters, and two launches
+    (128, 4, 1500, 300, 300, 200), (64, 3, 900, 500, 200, 450), (128, 2, 5000, 256, 256, 255), (64, 8, 700, 40, 40, 39),      # tiles of queries
+    (128, 4, 1100, 200, 30, 180), (64, 2, 3000, 64, 64, 0),                                # counted queries that stay, and the rows go by
+])
+def test_a_query_that_is_not_a_number_reaches_every_row_that_it_sees(cuda_lib, dtype, d, g, cap, m, n_scored, bad):
+    """What cannot be told comes out as NaN, like a wait that gives up: from a query's own output and the scores of all rows before its own,
+    and nowhere else."""
+    t, n = TYPES[dtype], cap - 3
+    k, v, q = _keys(1, 2, cap, d, dtype=t), _normal(2, 2, cap, d, dtype=t), _normal(3, 2, g, m, d, dtype=t)
+    clean = q[0].clone()
+    q[0, 0, bad, 5] = math.nan
+    out, score = cuda_lib.attn_scored(k, v, q, lens=_lens([n, n]), n_scored=n_scored)
+    sees = n - m + bad + 1
+    assert bool(out[0, 0, bad].isnan().all())
+    if bad >= m - n_scored:
+        assert bool(score[0, :sees].isnan().all()), int((~score[0, :sees].isnan()).sum())
+    else:
+        sees = 0
+    for s, queries in enumerate((clean, q[1])):
+        ref, got, tol, score_tol = scored(queries, k[s], v[s], n, None, n_scored, 1.0)
+        held = torch.ones(g, m, dtype=torch.bool, device="cuda")
+        held[0, bad] = s > 0
+        _near(out[s][held], ref[held], tol[held], ("out", s))
+        first = 0 if s else sees
+        _near(score[s, first:n], got[first:], score_tol[first:], ("score", s)) if first < n else None
