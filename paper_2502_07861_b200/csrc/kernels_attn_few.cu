@@ -633,6 +633,9 @@ __global__ void __launch_bounds__(32 * few_warps(kBf16, D), kCtas) attn_few_kern
   if (J.order == kFewBeside && blockIdx.x == gridDim.x - 1) grid_wait_and_release();
 }
 
+// A row's weight from its logit; a row that the query does not see has none, whatever the query's sum is.
+__device__ inline float logit_weight(float x, float lse) { return x == -INFINITY ? 0.f : exp2f(x - lse); }
+
 // The splits of a stream as a cluster of CTAs, where its logits fit their shared memory: they join their sums through it, every
 // CTA then turns its own logits into weights, and nothing but results leaves the chip.  More than eight query rows are groups with a
 // cluster each; what a cached row receives from a group goes to `sums` [groups, n_streams, cap] (one group: to the scores).
@@ -705,7 +708,7 @@ attn_few_cluster_kernel(const __grid_constant__ AttnRows A, const ScoreArgs S, i
   auto left = cluster.barrier_arrive();          // this CTA reads nobody's sums any more
   auto put = [&](int i, float before) {
     float sum = 0.f;
-    for (int r = 0; r < G.g; ++r) sum += exp2f(x[r * pitch + i - row0] - lse[r]);
+    for (int r = 0; r < G.g; ++r) sum += logit_weight(x[r * pitch + i - row0], lse[r]);
     if (sums) sums[(int64_t)group * A.n_streams * A.cap + first + i] = sum;
     else score_put(S, first + i, before, sum);
   };
@@ -792,7 +795,12 @@ __global__ void __launch_bounds__(kEndThreads, 4) few_end_kernel(const __grid_co
 #pragma unroll
   for (int j = 0; j < kPer; ++j) {
     const int key = k0 + tid + j * kEndThreads;
-    if (key < len) score_put(S, (int64_t)s * A.cap + key, old[j], sum[j]);
+    if (key >= len) continue;
+    if (sum[j] != sum[j]) {                      // some query's sum is not a number: whether this row is seen by it, from the logits again
+      sum[j] = 0.f;
+      for (int r = 0; r < A.n_rows; ++r) sum[j] += logit_weight(x[r * P.pitch + j * kEndThreads], lse[r]);
+    }
+    score_put(S, (int64_t)s * A.cap + key, old[j], sum[j]);
   }
 }
 

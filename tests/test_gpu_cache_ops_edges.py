@@ -41,7 +41,7 @@ def test_eviction_call_after_call_beside_other_work(cuda_lib, n_recent):
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("d,g,cap,m,n_scored,bad", [
-    (128, 4, 1000, 1, 1, 0), (64, 8, 9000, 1, 1, 0),                                        # one pass: clusters, and two launches
+    (128, 4, 1000, 1, 1, 0), (64, 8, 9000, 1, 1, 0), (64, 2, 40000, 3, 2, 1), (128, 2, 800, 4, 4, 2), (64, 3, 600, 33, 33, 20),      # one pass
     (128, 4, 1500, 300, 300, 200), (64, 3, 900, 500, 200, 450), (128, 2, 5000, 256, 256, 255), (64, 8, 700, 40, 40, 39),      # tiles of queries
     (128, 4, 1100, 200, 30, 180), (64, 2, 3000, 64, 64, 0),                                # counted queries that stay, and the rows go by
 ])
