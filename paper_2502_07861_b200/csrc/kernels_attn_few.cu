@@ -640,7 +640,10 @@ __device__ inline float logit_weight(float x, float lse) { return x == -INFINITY
 // CTA then turns its own logits into weights, and nothing but results leaves the chip.  More than eight query rows are groups with a
 // cluster each; what a cached row receives from a group goes to `sums` [groups, n_streams, cap] (one group: to the scores).
 constexpr int kMaxCluster = 8;
-constexpr int most_clustered(int C) { return C > 4 ? 192 : 256; }       // CTAs of a launch, by clusters of C
+// CTAs of a launch, by clusters of C, that all run at once: of fp32 rows with 128 dims, which have an SM to themselves, as many as the device takes (120
+// by clusters of 8, 132 by 4, 148; 64 streams of 250 such rows, 128 CTAs: 9.7 us in a graph against 11.6 by two launches, 80 of 200, 160 CTAs:
+// 16.9 against 13.0), of others two an SM, less than the 264 to 296 that it takes.
+constexpr int most_clustered(int C, bool alone) { return alone ? (C > 4 ? 120 : C > 2 ? 132 : 148) : C > 4 ? 192 : 256; }
 constexpr int logit_bytes(bool bf16, int d) { return !bf16 && d == 64 ? 8 * 1024 : 15 * 1024; }       // of a CTA: two (fp32, d = 128: one) still fit an SM
 
 template <bool kBf16, int D, int kR>
@@ -914,10 +917,12 @@ int few_splits(int64_t streams, int cap, int n_rows, int d, int is_bf16) {
 // rows in clusters of 16: 228 us against 108; 32 x 1024 rows by clusters of 8 12.4 us, of 4 8.7).
 int few_cluster(int64_t streams, int cap, int n_rows, int d, int is_bf16) {
   const int64_t sets = streams * ((n_rows + kFewRows - 1) / kFewRows);
+  const bool alone = !is_bf16 && d == 128;
+  static_assert(Few<false, 128>::kCtas == 1 && Few<false, 64>::kCtas == 2 && Few<true, 128>::kCtas == 2 && Few<true, 64>::kCtas == 2, "CTAs of a cluster that share an SM");
   int C = 1;
-  while (C < kMaxCluster && 2 * sets * C <= most_clustered(2 * C) && cap > C * kWarps * kTile) C *= 2;
+  while (C < kMaxCluster && 2 * sets * C <= most_clustered(2 * C, alone) && cap > C * kWarps * kTile) C *= 2;
   const int64_t rows = logit_pitch(cap, C);
-  return sets * C <= most_clustered(C) && std::min(n_rows, kFewRows) * rows * 4 <= logit_bytes(is_bf16, d) && rows * 2 * d * (is_bf16 ? 2 : 4) <= 256 << 10 ? C : 0;
+  return sets * C <= most_clustered(C, alone) && std::min(n_rows, kFewRows) * rows * 4 <= logit_bytes(is_bf16, d) && rows * 2 * d * (is_bf16 ? 2 : 4) <= 256 << 10 ? C : 0;
 }
 // Floats of the workspace that they need.
 int64_t few_cluster_sums(const AttnRows& A) { return A.n_rows > kFewRows ? (int64_t)(A.n_rows + kFewRows - 1) / kFewRows * A.n_streams * A.cap : 0; }

@@ -60,3 +60,17 @@ def test_a_cluster_barrier_comes_first(file, name, body):
 def test_an_access_behind_a_barrier_that_is_not_always_taken_is_found():
     assert _unguarded("{ if (a) { cluster.sync(); } cluster.map_shared_rank(p, 0); }")
     assert not _unguarded("{ if (a) { cluster.sync(); cluster.map_shared_rank(p, 0); } }")
+
+
+@pytest.mark.parametrize("streams,rows,bf16,clusters", [
+    (148, 120, 0, True), (74, 200, 0, True), (149, 120, 0, False), (200, 100, 0, False), (256, 60, 0, False), (80, 300, 0, False), (200, 100, 1, True), (256, 100, 1, True),
+])
+def test_clusters_serve_no_more_ctas_than_run_at_once(streams, rows, bf16, clusters):
+    """One query of up to eight heads over rows of 128 dims: the clusters need no workspace, two launches do.  A CTA of fp32 rows has an SM to itself."""
+    import ctypes as C
+
+    import paper_2502_07861_b200 as bk
+
+    size = C.c_size_t(0)
+    assert bk.load().balancekv_attn_scored_workspace(streams, rows, 1, 4, 128, bf16, 1, C.byref(size)) == 0
+    assert (size.value == 0) == clusters

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from cache_ops_util import scored
-from test_gpu_cache_ops import TYPES, _check_evict, _keys, _lens, _near, _normal
+from test_gpu_cache_ops import TYPES, _check_evict, _check_scored, _keys, _lens, _near, _normal
 
 pytestmark = pytest.mark.gpu
 
@@ -66,3 +66,8 @@ def test_a_query_that_is_not_a_number_reaches_every_row_that_it_sees(cuda_lib, d
         _near(out[s][held], ref[held], tol[held], ("out", s))
         first = 0 if s else sees
         _near(score[s, first:n], got[first:], score_tol[first:], ("score", s)) if first < n else None
+
+
+@pytest.mark.parametrize("streams,cap,g", [(200, 100, 4), (64, 500, 4), (40, 500, 8), (17, 900, 3), (148, 120, 2)])
+def test_fp32_streams_about_as_many_as_clusters_run_at_once(cuda_lib, streams, cap, g):
+    _check_scored(cuda_lib, "fp32", 128, g, cap, [cap - (13 * s) % 40 for s in range(streams)], 1, 1, seed=streams)
