@@ -163,7 +163,10 @@ def plan_calls(block: int, levels: int, recent_window: int, appended_after_event
 
 
 class Context:
-    """Owns one ``balancekv_ctx``.  Tensor arguments are CUDA torch tensors of the context's dtype."""
+    """Owns one ``balancekv_ctx``.  Tensor arguments are CUDA torch tensors of the context's dtype.
+
+    A call with ``stream=`` (a torch stream or a raw cudaStream_t) runs there and waits for no other stream: the caller orders it behind what makes
+    its tensors and keeps them until it is over."""
 
     def __init__(self, n_seqs=1, n_layers=1, n_kv_heads=1, n_q_heads=None, head_dim=128, dtype="bf16", block=1024,
                  levels=2, max_tokens=32768, max_pending=0, recent_window=0, center_keys=0, gram_path=0, seed=0,
@@ -502,12 +505,22 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _on_stream(stream):
-    """Tensors made inside belong to the stream of the call, so that their memory is not handed on while it still runs."""
+def _on_stream(stream, call, *tensors, **more):
+    """A call on a stream other than the current one.  Tensors made inside belong to that stream, and those given are recorded on it, so that the
+    memory of neither is handed on while the call still runs.  (A raw stream may be gone by the time that a tensor's memory is freed: there the
+    caller keeps the tensors.)"""
     torch = _torch()
-    if isinstance(stream, int):
+    raw = isinstance(stream, int)
+    if raw:
         stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
-    return torch.cuda.stream(stream)
+    with torch.cuda.stream(stream):
+        result = call(*tensors, **more)
+    if not raw:
+        out = more.get("out")
+        for t in (*tensors, *more.values(), *(out.values() if isinstance(out, dict) else ())):
+            if isinstance(t, torch.Tensor):
+                t.record_stream(stream)
+    return result
 
 
 @functools.lru_cache(maxsize=1024)
@@ -536,10 +549,13 @@ def attn_scored(K, V, q, lens=None, score=None, score_out=None, n_scored=None, d
     K, V: CUDA tensors [n_streams, capacity, d]; q: [n_streams, group, n_queries, d] or, for one query, [n_streams, group, d];
     lens: int32 [n_streams], rows in use (None: all).  The newest ``n_scored`` queries (None: all) add their weights to ``decay`` times
     ``score`` (float32 [n_streams, capacity]; None: zeros); the result goes to ``score_out``, by default ``score`` itself or a
-    new tensor of zeros.  Returns (out, score_out); with n_scored = 0 the second is ``score_out`` as it was."""
+    new tensor of zeros.  Returns (out, score_out); with n_scored = 0 the second is ``score_out`` as it was.
+
+    ``stream``: a torch stream or a raw cudaStream_t to run on in place of the current one.  The call does not wait for other streams: the caller orders
+    it behind what makes its tensors, and what uses its results behind it.  The tensors given may be let go once a call on a torch stream has
+    returned; for a raw one the caller keeps them until it is over.  (The same holds for cache_evict and decode_attn_prefix.)"""
     if stream is not None:
-        with _on_stream(stream):
-            return attn_scored(K, V, q, lens, score, score_out, n_scored, decay, out)
+        return _on_stream(stream, attn_scored, K, V, q, lens, score, score_out, n_scored=n_scored, decay=decay, out=out)
     what, torch = "balancekv_attn_scored", _torch()
     ks, qs = K.shape, q.shape
     if len(ks) != 3 or len(qs) not in (3, 4):
@@ -574,8 +590,7 @@ def cache_evict(K, V, score, n_keep, lens=None, pos=None, n_first=0, n_recent=0,
     fill, by default new tensors of min(n_keep, capacity) rows whose unused ones are zero; with ``in_place`` the cache itself, of which only
     the rows that fill a hole move (``pos`` and ``lens`` are updated if given, ``lens`` is made if not).  Returns that dict."""
     if stream is not None:
-        with _on_stream(stream):
-            return cache_evict(K, V, score, n_keep, lens, pos, n_first, n_recent, out, in_place)
+        return _on_stream(stream, cache_evict, K, V, score, n_keep, lens, pos, n_first=n_first, n_recent=n_recent, out=out, in_place=in_place)
     what, torch = "balancekv_cache_evict", _torch()
     ks = K.shape
     if len(ks) != 3:
@@ -622,8 +637,7 @@ def decode_attn_prefix(K_prefix, V_prefix, K, V, q, lens=None, weight=None, out=
     K, V: [n_seqs, n_kv_heads, capacity, d], or None where the sequences have no rows of their own; lens: int32 [n_seqs] (None: all rows
     are in use); q: [n_seqs, n_kv_heads * group, d]."""
     if stream is not None:
-        with _on_stream(stream):
-            return decode_attn_prefix(K_prefix, V_prefix, K, V, q, lens, weight, out)
+        return _on_stream(stream, decode_attn_prefix, K_prefix, V_prefix, K, V, q, lens, weight, out=out)
     what, torch = "balancekv_decode_attn_prefix", _torch()
     ps, qs = K_prefix.shape, q.shape
     if len(ps) != 3 or len(qs) != 3 or (K is None) != (V is None) or (K is not None and K.dim() != 4):

@@ -71,3 +71,54 @@ def test_a_query_that_is_not_a_number_reaches_every_row_that_it_sees(cuda_lib, d
 @pytest.mark.parametrize("streams,cap,g", [(200, 100, 4), (64, 500, 4), (40, 500, 8), (17, 900, 3), (148, 120, 2)])
 def test_fp32_streams_about_as_many_as_clusters_run_at_once(cuda_lib, streams, cap, g):
     _check_scored(cuda_lib, "fp32", 128, g, cap, [cap - (13 * s) % 40 for s in range(streams)], 1, 1, seed=streams)
+
+
+def _busy(stream, cycles=60_000_000):
+    """Some 30 ms of work ahead of what comes next on the stream."""
+    with torch.cuda.stream(stream):
+        torch.cuda._sleep(cycles)
+
+
+def test_tensors_let_go_while_a_call_on_another_stream_waits(cuda_lib):
+    """Temporaries passed with ``stream=``: their memory goes to nobody else before the call is over."""
+    bk, side, t = cuda_lib, torch.cuda.Stream(), torch.bfloat16
+    sizes = [(6, 700, 128), (6, 700, 128), (6, 4, 20, 128), (6, 700), (3, 2, 700, 128), (3, 2, 700, 128), (3, 8, 128)]
+
+    def calls(stream=None):
+        k, v, q, score, k2, v2, q2 = (_normal(i, *size, dtype=torch.float32 if len(size) == 2 else t) for i, size in enumerate(sizes))
+        lens, w = _lens([700, 3, 0, 650, 128, 77]), _normal(9, 6, 700).abs()[:2].contiguous()
+        torch.cuda.synchronize()
+        if stream is not None:
+            _busy(stream)
+        out, new = bk.attn_scored(k, v, q, lens=lens, score=score, score_out=torch.zeros(6, 700, device="cuda"), stream=stream)
+        torch.cuda.current_stream().synchronize()          # (score_out's zeros)
+        if stream is not None:
+            _busy(stream)
+        kept = bk.cache_evict(k, v, score, 100, lens=lens, pos=_lens(list(range(4200))).view(6, 700), stream=stream)
+        return [out, new, *kept.values(), bk.decode_attn_prefix(k[:2], v[:2], k2, v2, q2, weight=w, stream=stream)]
+
+    want = calls()
+    torch.cuda.synchronize()
+    want = [x.clone() for x in want]
+    got = calls(side)
+    noise = [torch.full(size, float("nan"), device="cuda", dtype=dtype) for size in [*sizes, (6,), (6, 700), (2, 700)] for dtype in (t, torch.float32) for _ in range(4)]
+    torch.cuda.synchronize()
+    del noise
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_a_call_on_a_stream_within_a_capture(cuda_lib):
+    bk, side = cuda_lib, torch.cuda.Stream()
+    k, v, q = _normal(1, 4, 900, 64), _normal(2, 4, 900, 64), _normal(3, 4, 2, 64)
+    want = [x.clone() for x in bk.attn_scored(k, v, q)]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        here = torch.cuda.current_stream()
+        side.wait_stream(here)
+        got = bk.attn_scored(k, v, q, stream=side)
+        here.wait_stream(side)
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
