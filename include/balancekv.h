@@ -207,7 +207,11 @@ int balancekv_decode_attn_static_status(int* status_host, void* stream);
  * _workspace call of the same arguments gives on the host; contents need not be kept or cleared).  Calls that may overlap, graph replays
  * among them, need workspaces of their own.  Nothing is allocated and nothing synchronised; every call may be captured.
  * Device-side waits are bounded; should one give up, the floating-point results of its launch are NaN.  Memory that a
- * call writes overlaps nothing else that it is given, unless stated.  Errors: BALANCEKV_E_INVAL for bad arguments,
+ * call writes overlaps nothing else that it is given, unless stated.
+ * Logits, softmax statistics, partial results and scores are float32, and each output is rounded to dtype once.  In bfloat16 the
+ * weights that multiply V are held in 16 bits by calls of up to eight query rows a stream (group * n_queries; behind a prefix
+ * n_seqs * group, own rows always); of more they are rounded to bfloat16, each by up to 2^-8 of itself (their sum is not): an output
+ * of such a call is off by up to 2^-8 sum_i p_i |v_i| beside its own rounding.  Errors: BALANCEKV_E_INVAL for bad arguments,
  * BALANCEKV_E_NOMEM for too small a workspace, BALANCEKV_E_CUDA. */
 
 /* Attention of the newest n_queries tokens of every stream over its cache, and the weight that each cached row receives:
@@ -217,7 +221,8 @@ int balancekv_decode_attn_static_status(int* status_host, void* stream);
  * The last n_queries rows in use are the queries' own tokens, in order: query j sees the rows up to its own (one query: all of
  * them).  A query ahead of the first row (len < n_queries, a padded sequence) sees nothing: its output is zero.
  * K, V: [n_streams, capacity, head_dim]   q, out: [n_streams, group, n_queries, head_dim]   score_in (may be NULL: zeros),
- * score_out (may be score_in): float32 [n_streams, capacity]; scores behind the last row stay as they are.  n_scored: the newest queries
+ * score_out (may be score_in): float32 [n_streams, capacity]; scores behind the last row stay as they are (so a row that
+ * is appended has the score that its place held: the caller sets it).  n_scored: the newest queries
  * that count, 0 .. n_queries; with 0 the scores are not touched and may be NULL. */
 int balancekv_attn_scored(const void* K, const void* V, const int32_t* lens, int n_streams, int capacity, const void* q, void* out,
                           int n_queries, int group, int head_dim, int dtype, const float* score_in, float* score_out, int n_scored,

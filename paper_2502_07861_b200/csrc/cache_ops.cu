@@ -91,11 +91,12 @@ bool prefix_by_few(const AttnRows& P, int dtype) { return P.n_rows <= (dtype ? k
 // that works.  Times in us: a pair of query tiles with a tile of keys takes 1.7, a tile of keys by itself 1.55 (it waits for memory); the one-pass
 // kernel reads 6 MB and a wave of its CTAs takes 4.5.  The SMs are shared out by these times, the tensor-core kernel's counted half as long
 // again, since others now read too, the own rows' at half of their capacity, which is what they fill on the way; three quarters at most (128 x 8 x 4
-// behind 16384 rows, 300 own each: 55 us by 112 CTAs, 69 by 128).  256 sequences x 5 heads x 8 behind 8192 rows: with 1024 own rows each
-// 210 us one after the other, 192 so, with up to 1024 146 and 129, with 256 116 and 91.
+// behind 16384 rows, 300 own each: 66 to 71 us by 112 CTAs, 84 by 128, 74 one after the other; up to 300: 64, 68, 62).  Calls one behind the
+// other, on three sets of inputs in turn: 256 sequences x 5 heads x 8 behind 8192 rows with 1024 own rows each 220 us one after the other, 193 so,
+// with up to 1024 147 and 137, with 256 113 and 104, with up to 256 96 and 101.
 // It costs a launch that joins, unless the own rows need one anyway: short ones finish the outputs themselves instead (64 x 4 x 8 behind 32768
-// rows, 200 own: 52 us against 55), and where the tensor-core kernel waits for memory too, so do all that are not most of the work (32 x 4 x 8
-// behind 32768, 512 own: 44 and 48; 2048 own: 83 and 74).
+// rows, 200 own: 60 us against 62 beside), and where the tensor-core kernel waits for memory too, so do all that are not most of the work (32 x 4 x 8
+// behind 32768, 512 own: 45 against 51 beside; 2048 own: 85 against 75).
 bool prefix_beside(const AttnRows& P, const AttnRows& A, int head_dim, int& splits) {
   const bool by_keys = attn_tc_by_keys(P);
   const int64_t blocks = attn_tc_blocks(P), tiles = (P.cap + 127) / 128;
