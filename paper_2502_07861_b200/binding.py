@@ -507,11 +507,11 @@ def _ptr(t):
 
 def _on_stream(stream, call, *tensors, **more):
     """A call on a stream other than the current one.  Tensors made inside belong to that stream, and those given are recorded on it, so that the
-    memory of neither is handed on while the call still runs.  (A raw stream may be gone by the time that a tensor's memory is freed: there the
-    caller keeps the tensors.)"""
+    memory of neither is handed on while the call still runs.  (A raw stream, or torch's ExternalStream of one, may be gone by the time that a
+    tensor's memory is freed: there the caller keeps the tensors.)"""
     torch = _torch()
-    raw = isinstance(stream, int)
-    if raw:
+    raw = isinstance(stream, (int, torch.cuda.ExternalStream))
+    if isinstance(stream, int):
         stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
     with torch.cuda.stream(stream):
         result = call(*tensors, **more)
@@ -553,7 +553,7 @@ def attn_scored(K, V, q, lens=None, score=None, score_out=None, n_scored=None, d
 
     ``stream``: a torch stream or a raw cudaStream_t to run on in place of the current one.  The call does not wait for other streams: the caller orders
     it behind what makes its tensors, and what uses its results behind it.  The tensors given may be let go once a call on a torch stream has
-    returned; for a raw one the caller keeps them until it is over.  (The same holds for cache_evict and decode_attn_prefix.)"""
+    returned; for a raw one (an ExternalStream too) the caller keeps them until it is over.  (The same holds for cache_evict and decode_attn_prefix.)"""
     if stream is not None:
         return _on_stream(stream, attn_scored, K, V, q, lens, score, score_out, n_scored=n_scored, decay=decay, out=out)
     what, torch = "balancekv_attn_scored", _torch()

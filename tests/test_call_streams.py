@@ -11,11 +11,18 @@ class _Stream:
     cuda_stream = 5
 
 
+class _External(_Stream):
+    """A stream that somebody else made, and may have destroyed when a tensor's memory is freed."""
+
+    def __init__(self, handle):
+        self.cuda_stream = handle
+
+
 @pytest.fixture
 def recorded(monkeypatch):
     seen = []
     monkeypatch.setattr(torch.cuda, "stream", lambda stream: contextlib.nullcontext())
-    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle: handle)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", _External)
     monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, stream: seen.append((t, stream)))
     return seen
 
@@ -61,5 +68,6 @@ def test_nothing_is_recorded_on_a_raw_stream_or_the_current_one(monkeypatch, rec
     _launches_nothing(monkeypatch)
     call, _ = _calls()[which]
     call(5)
+    call(_External(5))
     call(None)
     assert not recorded
